@@ -389,6 +389,121 @@ mp_status mp_manifest_threshold_reads(const mp_manifest* man, uint64_t* bytes);
    when the family gave none).  Host only; no device wait. */
 mp_status mp_manifest_lineage(const mp_manifest* man, uint64_t* ids);
 
+/*
+ * Layer operators: what a merged checkpoint's layers compute, and what a loss says about its weights and
+ * about the merge coefficients.  They hold no handle: scratch comes from the library's pool in
+ * stream order and goes back likewise, so that calls on any streams do not meet.  They can be
+ * captured into CUDA graphs like the calls above.  Matrices are device memory, row-major with a row
+ * stride; every matrix and vector of a call has the call's dtype (bf16 or fp32) except the fp32
+ * statistics.  Sums, statistics and products are held in fp32, and each output element is rounded
+ * once (linear_backward also rounds dz, an operand of its products, to dtype).  Outputs must not overlap
+ * another argument, except the pairs named below, which may be the same matrix; columns
+ * of one wider matrix side by side do not overlap.  rows may be 0: then nothing is computed,
+ * and sums over rows are 0.  A kernel's bounded wait that gives up (which nothing but the test hook
+ * is known to cause) is reported by mp_layer_status.
+ */
+typedef struct {
+  void* data;  /* element (r, c) at data + r * ld + c; NULL: absent */
+  uint64_t ld; /* elements from one row to the next, >= the columns (not looked at with one row) */
+} mp_matrix;
+
+typedef enum { MP_NORM_RMS = 0, MP_NORM_LAYER = 1 } mp_norm_kind;
+typedef enum { MP_ACT_NONE = 0, MP_ACT_RELU = 1, MP_ACT_SILU = 2, MP_ACT_GELU = 3, MP_ACT_GELU_TANH = 4 } mp_act;
+
+/*
+ * mp_norm — layer norm or RMS norm of every row of x [rows][cols]:
+ *   mu = mean(x) (LAYER; 0 for RMS), v = mean((x - mu)^2), rstd = 1 / sqrt(v + eps),
+ *   y = (x - mu) * rstd * weight + bias.
+ * weight and bias [cols] may be NULL (1 and 0); mean and rstd [rows], fp32, what the backward pass needs, may
+ * be NULL.  RMS has no bias and no mean.  A row is read before it is written: y may be x.
+ * Errors: MP_ERR_INVALID_ARG, MP_ERR_CUDA.
+ */
+typedef struct {
+  mp_dtype dtype;
+  mp_norm_kind kind;
+  uint64_t rows, cols; /* cols in [1, 2^28] */
+  float eps;           /* finite, >= 0 */
+  mp_matrix x, y;
+  const void *weight, *bias;
+  float *mean, *rstd;
+} mp_norm_args;
+mp_status mp_norm(const mp_norm_args* args, mp_stream stream);
+
+/*
+ * mp_norm_backward — the gradients of mp_norm from dy and the forward pass's statistics.  With
+ * xh = (x - mean) * rstd and g = dy * weight:
+ *   dx = rstd * (g - mean(g) [LAYER] - xh * mean(g * xh)) + add,
+ *   dweight = sum over rows of dy * xh,  dbias = sum over rows of dy.
+ * Outputs that are NULL are not computed; add (NULL: 0) is the gradient that reaches x by another
+ * way, such as the residual stream's, and may be dx.  The sums over rows are taken in a fixed order:
+ * the same call gives the same bits.  Errors: MP_ERR_INVALID_ARG, MP_ERR_OOM, MP_ERR_CUDA.
+ */
+typedef struct {
+  mp_dtype dtype;
+  mp_norm_kind kind;
+  uint64_t rows, cols;
+  mp_matrix dy, x, add, dx;
+  const void* weight;
+  const float *mean, *rstd;
+  void *dweight, *dbias;
+} mp_norm_backward_args;
+mp_status mp_norm_backward(const mp_norm_backward_args* args, mp_stream stream);
+
+/*
+ * mp_linear — y = act(z) * mul + residual with z = x w^T + bias, for x [rows][in], w [out][in] (as checkpoints
+ * hold it), bias [out], and mul, residual, y [rows][out].  bias, mul and residual may be absent; pre
+ * [rows][out], where given, receives z for the backward pass.  y may be mul or residual.  GELU is
+ * the one with the error function, GELU_TANH its approximation by tanh.  From one row (a single
+ * token) on; a bf16 operand whose rows are not whole 16-byte vectors is copied to scratch first.
+ * Errors: MP_ERR_INVALID_ARG, MP_ERR_UNSUPPORTED, MP_ERR_OOM, MP_ERR_CUDA.
+ */
+typedef struct {
+  mp_dtype dtype;
+  mp_act act;
+  uint64_t rows, in, out; /* in and out in [1, 2^31 - 256] */
+  mp_matrix x, w, mul, residual, y, pre;
+  const void* bias;
+} mp_linear_args;
+mp_status mp_linear(const mp_linear_args* args, mp_stream stream);
+
+/*
+ * mp_linear_backward — the gradients of mp_linear from dy [rows][out].  With dz = dy * mul * act'(pre):
+ *   dx = dz w + dx_add,  dw = dz^T x + dw_add,  db = sum over rows of dz,  dmul = dy * act(pre);
+ * the residual's gradient is dy itself.  Outputs that are NULL are not computed, and what only they
+ * need may be absent (w for dx, x for dw).  pre is needed with an activation and for dmul.
+ * dx_add and dw_add (NULL: 0) may be dx and dw: gradients that add up.  Sums are taken in a fixed
+ * order.  Errors: as mp_linear.
+ */
+typedef struct {
+  mp_dtype dtype;
+  mp_act act;
+  uint64_t rows, in, out;
+  mp_matrix dy, x, w, pre, mul, dx_add, dw_add, dx, dw, dmul;
+  void* db;
+} mp_linear_backward_args;
+mp_status mp_linear_backward(const mp_linear_backward_args* args, mp_stream stream);
+
+/*
+ * mp_coef_grad — the gradient of a loss with respect to the merge coefficients, per expert and tensor:
+ *   out[i][t] = sum over the blocks b of tensor t with A_{i,b} = 1 of sum_j grad[j] * (M_i[j] - M_0[j]),
+ * where grad is the loss's gradient with respect to the merged weights (a device buffer of the family's dtype laid
+ * out like the base, 16-byte aligned).  With M_A = M_0 + sum_i alpha_i A_i Delta_i (AVG, TA; Prop. 2)
+ * summing row i over the tensors gives dL / dalpha_i; the entries themselves are the
+ * gradients of coefficients per tensor.  Only the plan's blocks are read (non-anticipatory, like the merge), and
+ * gradients are taken straight through the rounding of the merged weights.  out: device, fp32
+ * [K][n_tensors].  The plan's operator must be AVG or TA (MP_ERR_UNSUPPORTED for the others, whose
+ * output is not linear in alpha), the experts in device memory (MP_ERR_UNSUPPORTED for a host-resident pool).  Sums: fp32
+ * within 16 KiB of a block, fp64 over those, in a fixed order.
+ * Errors: MP_ERR_INVALID_ARG, MP_ERR_MISMATCH, MP_ERR_UNSUPPORTED, MP_ERR_OOM, MP_ERR_CUDA.
+ */
+mp_status mp_coef_grad(const mp_family* family, const mp_index* index, const mp_plan_t* plan, const void* grad,
+                       float* out, mp_stream stream);
+
+/* Waits for the stream, then reports what layer operators (on any stream) met since the last
+   such call: MP_OK, or MP_ERR_TIMEOUT when a bounded device wait gave up (its call's outputs are
+   unspecified). */
+mp_status mp_layer_status(mp_stream stream);
+
 /* B = floor(f * C_full) with C_full = K * sum_t numel_t * element size (the full expert
    read); f in [0, 1] (clamped).  Returns 0 for an invalid family. */
 uint64_t mp_budget_from_fraction(const mp_family* family, double f);
@@ -409,7 +524,8 @@ uint64_t mp_kernel_launch_count(void);
  * mp_trace_start(capacity): from now on every call records the device time of its work
  * as ranges of two CUDA events, on the stream that runs it, until capacity ranges are
  * held: one range per mp_index_blocks (MP_TRACE_INDEX), mp_plan (MP_TRACE_PLAN) and
- * mp_merge / mp_merge_touched (MP_TRACE_MERGE) on the caller's stream, and, for experts in
+ * mp_merge / mp_merge_touched (MP_TRACE_MERGE), mp_norm / mp_norm_backward (MP_TRACE_NORM), mp_linear /
+ * mp_linear_backward (MP_TRACE_LINEAR) and mp_coef_grad (MP_TRACE_COEF) on the caller's stream, and, for experts in
  * pinned host memory, one range per segment for its gather on the side stream
  * (MP_TRACE_GATHER) and for its kernels on the caller's stream (MP_TRACE_SEGMENT).  A
  * start while a trace is held discards it.  Returns MP_ERR_INVALID_ARG for capacity 0 or
@@ -426,6 +542,9 @@ uint64_t mp_kernel_launch_count(void);
 #define MP_TRACE_MERGE 3
 #define MP_TRACE_GATHER 4
 #define MP_TRACE_SEGMENT 5
+#define MP_TRACE_NORM 6
+#define MP_TRACE_LINEAR 7
+#define MP_TRACE_COEF 8
 typedef struct mp_trace_range {
   uint32_t kind;     /* MP_TRACE_* */
   uint32_t segment;  /* host-pool segment (GATHER, SEGMENT), else 0 */
@@ -457,14 +576,14 @@ mp_status mp_trace_read(mp_trace_range* out, uint64_t n);
  * mp_last_error() then names the injected fault.  Returns MP_ERR_INVALID_ARG for an unknown
  * kind.
  *
- * mp_debug_stall_pipeline(rounds): the index and merge kernels launched from now on never arm
+ * mp_debug_stall_pipeline(rounds): the index, merge and (bf16) linear kernels launched from now on never arm
  * the first slot of each CTA's shared-memory ring (its bulk copy is not issued), so the
  * consumers' wait for it cannot complete, and every pipeline wait (producer or consumer
  * mbarrier) gives up after `rounds` polling rounds instead of the default 2^21; in mp_plan calls of
  * more than 2^17 units one CTA of the planner's grid never comes to its barrier, where the
  * others give up after `rounds` polls.  The wait
  * that runs out sets the handle's error word; the accessors of that handle and of the
- * handles built from it return MP_ERR_TIMEOUT.  The waits that drain a CTA's own bulk
+ * handles built from it (for linear layers mp_layer_status) return MP_ERR_TIMEOUT.  The waits that drain a CTA's own bulk
  * copies before it exits keep the full limit, so no copy is in flight when a kernel
  * returns.  rounds = 0 turns the stall off.
  */

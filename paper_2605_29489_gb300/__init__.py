@@ -31,6 +31,9 @@ __all__ = [
     "MP_FAULT_ALLOC", "MP_FAULT_GATHER", "MP_FAULT_CLUSTER", "mp_debug_inject_fault", "mp_debug_stall_pipeline",
     "MP_TRACE_INDEX", "MP_TRACE_PLAN", "MP_TRACE_MERGE", "MP_TRACE_GATHER", "MP_TRACE_SEGMENT",
     "mp_trace_start", "mp_trace_stop", "library_path",
+    "MP_NORM_RMS", "MP_NORM_LAYER", "MP_ACT_NONE", "MP_ACT_RELU", "MP_ACT_SILU", "MP_ACT_GELU", "MP_ACT_GELU_TANH",
+    "mp_norm", "mp_norm_backward", "mp_linear", "mp_linear_backward", "mp_coef_grad", "mp_layer_status",
+    "MP_TRACE_NORM", "MP_TRACE_LINEAR", "MP_TRACE_COEF",
 ]
 
 MP_OK = 0
@@ -42,6 +45,9 @@ MP_NNZ_MISSING = 0xFFFFFFFF   # catalog entry without block statistics (tensor-l
 MP_FAULT_ALLOC, MP_FAULT_GATHER, MP_FAULT_CLUSTER = 1, 2, 3  # test hooks: kinds of injected host-side failures
 # kinds of traced device-time ranges (mp_trace_start)
 MP_TRACE_INDEX, MP_TRACE_PLAN, MP_TRACE_MERGE, MP_TRACE_GATHER, MP_TRACE_SEGMENT = 1, 2, 3, 4, 5
+MP_TRACE_NORM, MP_TRACE_LINEAR, MP_TRACE_COEF = 6, 7, 8
+MP_NORM_RMS, MP_NORM_LAYER = 0, 1
+MP_ACT_NONE, MP_ACT_RELU, MP_ACT_SILU, MP_ACT_GELU, MP_ACT_GELU_TANH = 0, 1, 2, 3, 4
 
 
 class MergePipeError(RuntimeError):
@@ -71,6 +77,26 @@ class _Op(ctypes.Structure):
                 ("density", ctypes.c_float), ("trim_scope", ctypes.c_uint32), ("drop_p", ctypes.c_double),
                 ("seed", ctypes.c_uint64), ("score_mode", ctypes.c_uint32)]
 
+
+def _struct(name, *fields):
+    """a Structure of ints (i), uint64s (u), floats (f), pointers (p) and matrices (m: pointer, row stride)"""
+    flat = []
+    for kind, names in fields:
+        for n in names.split():
+            if kind == "m":
+                flat += [(n, ctypes.c_void_p), ("ld" + n, ctypes.c_uint64)]
+            else:
+                flat.append((n, {"i": ctypes.c_int, "u": ctypes.c_uint64, "f": ctypes.c_float, "p": ctypes.c_void_p}[kind]))
+    return type(name, (ctypes.Structure,), {"_fields_": flat})
+
+
+_NormArgs = _struct("_NormArgs", ("i", "dtype kind"), ("u", "rows cols"), ("f", "eps"), ("m", "x y"),
+                    ("p", "weight bias mean rstd"))
+_NormBackwardArgs = _struct("_NormBackwardArgs", ("i", "dtype kind"), ("u", "rows cols"), ("m", "dy x add dx"),
+                            ("p", "weight mean rstd dweight dbias"))
+_LinearArgs = _struct("_LinearArgs", ("i", "dtype act"), ("u", "rows in_ out"), ("m", "x w mul residual y pre"), ("p", "bias"))
+_LinearBackwardArgs = _struct("_LinearBackwardArgs", ("i", "dtype act"), ("u", "rows in_ out"),
+                              ("m", "dy x w pre mul dx_add dw_add dx dw dmul"), ("p", "db"))
 
 _lib = None
 
@@ -105,6 +131,12 @@ def lib():
             ("mp_manifest_info", [vp, vp, vp, vp, vp]),
             ("mp_manifest_lineage", [vp, vp]),
             ("mp_manifest_threshold_reads", [vp, vp]),
+            ("mp_norm", [vp, vp]),
+            ("mp_norm_backward", [vp, vp]),
+            ("mp_linear", [vp, vp]),
+            ("mp_linear_backward", [vp, vp]),
+            ("mp_coef_grad", [vp, vp, vp, vp, vp, vp]),
+            ("mp_layer_status", [vp]),
         ]:
             f = getattr(L, name)
             f.restype, f.argtypes = st, args
@@ -428,3 +460,155 @@ def mp_plan_noalloc(K, n_blocks, n_groups, dtype, blk_len, blk_group, norm, maxa
     _check(L.mp_plan_noalloc(K, n_blocks, n_groups, dtype, opt(blk_len), opt(blk_group), opt(norm), opt(maxabs),
                              opt(nnz), opt(tau), opt(index_err), op.ref(), int(budget_bytes), opt(mask), opt(order),
                              opt(summary), ctypes.c_void_p(_stream_ptr(stream))))
+
+
+# ---- layer operators --------------------------------------------------------------------------------
+
+
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return MP_BF16
+    if t.dtype == torch.float32:
+        return MP_F32
+    raise ValueError(f"layer operators take bfloat16 or float32 tensors, not {t.dtype}")
+
+
+def _matrix(name, t, shape, like):
+    """(address, row stride) of a 2-d tensor of the given shape with contiguous rows; (None, 0) for None"""
+    if t is None:
+        return None, 0
+    if t.shape != shape or t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} of {like.dtype}, not {tuple(t.shape)} of {t.dtype}")
+    _on_device(name, t, like)
+    rows, cols = shape
+    row, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    return t.data_ptr(), row if rows > 1 else cols
+
+
+def _on_device(name, t, like):
+    if not t.is_cuda or t.device != like.device:
+        raise ValueError(f"{name} must be on the device of the other tensors, a GPU")
+
+
+def _vector(name, t, n, like, dtype=None):
+    if t is None:
+        return None
+    if t.shape != (n,) or t.dtype != (dtype or like.dtype) or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be {n} contiguous elements of {dtype or like.dtype}")
+    _on_device(name, t, like)
+    return t.data_ptr()
+
+
+def _two_d(name, t):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    return t.shape
+
+
+def _call(f, args, stream):
+    rc = f(ctypes.byref(args), _stream_ptr(stream))
+    if rc != MP_OK:
+        _check(rc)
+
+
+def mp_norm(x, weight=None, bias=None, eps=1e-6, kind=MP_NORM_RMS, out=None, stream=None):
+    """(y, mean, rstd): layer norm or RMS norm of the rows of x [rows, cols]; mean is None for MP_NORM_RMS.
+    out: where y goes (may be x), else a new tensor"""
+    import torch
+    shape = _two_d("x", x)
+    rows, cols = shape
+    layer = kind == MP_NORM_LAYER
+    y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    mean = torch.empty(rows, dtype=torch.float32, device=x.device) if layer else None
+    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _call(lib().mp_norm,
+          _NormArgs(_dtype_of(x), kind, rows, cols, eps, *_matrix("x", x, shape, x), *_matrix("out", y, shape, x),
+                    _vector("weight", weight, cols, x), _vector("bias", bias, cols, x),
+                    mean.data_ptr() if layer else None, rstd.data_ptr()), stream)
+    return y, mean, rstd
+
+
+def mp_norm_backward(dy, x, weight, mean, rstd, kind=MP_NORM_RMS, bias=False, add=None, dx=None, stream=None):
+    """(dx, dweight, dbias) of mp_norm; dweight is None without a weight, dbias unless `bias` is set.  add: a
+    gradient that reaches x by another way, added to dx; dx: where it goes (may be add), else a new tensor"""
+    import torch
+    shape = _two_d("x", x)
+    rows, cols = shape
+    if dx is None:
+        dx = torch.empty(shape, dtype=x.dtype, device=x.device)
+    dw = None if weight is None else torch.empty(cols, dtype=x.dtype, device=x.device)
+    db = torch.empty(cols, dtype=x.dtype, device=x.device) if bias else None
+    _call(lib().mp_norm_backward,
+          _NormBackwardArgs(_dtype_of(x), kind, rows, cols, *_matrix("dy", dy, shape, x), *_matrix("x", x, shape, x),
+                            *_matrix("add", add, shape, x), *_matrix("dx", dx, shape, x), _vector("weight", weight, cols, x),
+                            _vector("mean", mean, rows, x, torch.float32), _vector("rstd", rstd, rows, x, torch.float32),
+                            None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()), stream)
+    return dx, dw, db
+
+
+def mp_linear(x, w, bias=None, act=MP_ACT_NONE, mul=None, residual=None, keep_pre=False, out=None, stream=None):
+    """(y, pre): y = act(z) * mul + residual, z = x w^T + bias, for x [rows, in] and w [out, in]; pre is z where
+    keep_pre is set (the backward pass needs it with an activation or a factor), else None.  out: where y goes
+    (may be mul or residual), else a new tensor"""
+    import torch
+    rows, k = xs = _two_d("x", x)
+    n = _two_d("w", w)[0]
+    shape = (rows, n)
+    y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    pre = torch.empty(shape, dtype=x.dtype, device=x.device) if keep_pre else None
+    _call(lib().mp_linear,
+          _LinearArgs(_dtype_of(x), act, rows, k, n, *_matrix("x", x, xs, x), *_matrix("w", w, (n, k), x),
+                      *_matrix("mul", mul, shape, x), *_matrix("residual", residual, shape, x), *_matrix("out", y, shape, x),
+                      *_matrix("pre", pre, shape, x), _vector("bias", bias, n, x)), stream)
+    return y, pre
+
+
+def mp_linear_backward(dy, x, w, pre=None, act=MP_ACT_NONE, mul=None, bias=False, need_dx=True, need_dw=True, dx_add=None,
+                       dw_add=None, dx=None, dw=None, stream=None):
+    """(dx, dw, db, dmul) of mp_linear; db only where `bias` is set, dmul with a factor.  dx_add, dw_add: gradients
+    to add to; dx, dw: where the results go (may be dx_add and dw_add), else new tensors"""
+    import torch
+    rows, k = xs = _two_d("x", x)
+    n = _two_d("w", w)[0]
+    ws, shape = (n, k), (rows, n)
+    if not need_dx:
+        dx = dx_add = None
+    elif dx is None:
+        dx = torch.empty(xs, dtype=x.dtype, device=x.device)
+    if not need_dw:
+        dw = dw_add = None
+    elif dw is None:
+        dw = torch.empty(ws, dtype=x.dtype, device=x.device)
+    db = torch.empty(n, dtype=x.dtype, device=x.device) if bias else None
+    dmul = None if mul is None else torch.empty(shape, dtype=x.dtype, device=x.device)
+    _call(lib().mp_linear_backward,
+          _LinearBackwardArgs(_dtype_of(x), act, rows, k, n, *_matrix("dy", dy, shape, x), *_matrix("x", x, xs, x),
+                              *_matrix("w", w, ws, x), *_matrix("pre", pre, shape, x), *_matrix("mul", mul, shape, x),
+                              *_matrix("dx_add", dx_add, xs, x), *_matrix("dw_add", dw_add, ws, x),
+                              *_matrix("dx", dx, xs, x), *_matrix("dw", dw, ws, x), *_matrix("dmul", dmul, shape, x),
+                              None if db is None else db.data_ptr()), stream)
+    return dx, dw, db, dmul
+
+
+def mp_coef_grad(fam: Family, index: Handle, plan: Handle, grad, out=None, stream=None):
+    """[K, n_tensors] fp32: the gradient of the merge coefficients from the gradient of the merged weights (a flat tensor
+    laid out like the base), over the blocks that the plan reads; its rows' sums are dL / dalpha.  AVG and TA"""
+    import torch
+    shape = (fam.K, len(fam.tensors))
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=grad.device)
+    elif out.shape != shape or out.dtype != torch.float32 or not out.is_contiguous():
+        raise ValueError(f"out must be {shape} contiguous elements of float32")
+    span = fam.tensors[-1][0] + fam.tensors[-1][1]
+    if _dtype_of(grad) != fam.c.dtype or not grad.is_contiguous() or grad.numel() < span:
+        raise ValueError("grad must be a contiguous tensor of the family's type that spans its tensors")
+    _check(lib().mp_coef_grad(fam.ref(), index.ptr, plan.ptr, grad.data_ptr(), out.data_ptr(), _stream_ptr(stream)))
+    return out
+
+
+def mp_layer_status(stream=None):
+    """wait for the stream; raises if a bounded wait of a layer operator gave up since the last call"""
+    _check(lib().mp_layer_status(_stream_ptr(stream)))

@@ -13,7 +13,7 @@
 #include <string>
 #include <vector>
 
-#include "mp_internal.cuh"
+#include "layer.cuh"
 
 namespace mp {
 
@@ -343,6 +343,25 @@ void set_error(const std::string& msg) {
 void set_static_error(const char* msg) { g_static_error = msg; }
 
 bool cluster_refused() { return inject_fault(MP_FAULT_CLUSTER); }
+
+cudaError_t scratch_alloc(void** p, size_t bytes, cudaStream_t st) { return malloc_async(p, bytes, st); }
+
+void scratch_free(void* p, cudaStream_t st) {
+  if (cudaFreeAsync(p, st) != cudaSuccess) cudaGetLastError();
+}
+
+bool device_pointer(const void* p) { return is_device_ptr(p); }
+
+uint32_t* layer_error_word() {
+  static uint32_t* const word = [] {
+    uint32_t* w = static_cast<uint32_t*>(pin_get(256));
+    if (w) *w = 0;
+    return w;
+  }();
+  return word;
+}
+
+uint32_t stall_rounds() { return g_stall_rounds.load(std::memory_order_relaxed); }
 
 void count_launches(uint64_t n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 
@@ -1492,6 +1511,79 @@ mp_status mp_merge(const mp_family* family, const mp_index* index, const mp_plan
 mp_status mp_merge_touched(const mp_family* family, const mp_index* index, const mp_plan_t* plan, void* out_buf,
                            mp_stream stream, mp_manifest** man_out) {
   return merge_common(family, index, plan, out_buf, stream, man_out, true);
+}
+
+mp_status mp_coef_grad(const mp_family* family, const mp_index* index, const mp_plan_t* plan, const void* grad,
+                       float* out, mp_stream stream) {
+  NvtxScope nv("mp_coef_grad");
+  mp_status st;
+  if ((st = check_handle(index, kMagicIndex, "index")) != MP_OK) return st;
+  if ((st = check_handle(plan, kMagicPlan, "plan")) != MP_OK) return st;
+  if (plan->index_id != index->id) return fail(MP_ERR_MISMATCH, "plan was built from a different index");
+  Geometry g;
+  if ((st = build_geometry(family, g)) != MP_OK) return st;
+  if (!g.same_as(index->g)) return fail(MP_ERR_MISMATCH, "family geometry differs from the index's");
+  if (plan->op_kind != MP_OP_AVG && plan->op_kind != MP_OP_TA)
+    return fail(MP_ERR_UNSUPPORTED, "coefficient gradients need a plan of AVG or TA");
+  if (family->experts_location != 0)
+    return fail(MP_ERR_UNSUPPORTED, "coefficient gradients need experts in device memory");
+  if (!grad || reinterpret_cast<uintptr_t>(grad) % 16 != 0 || !is_device_ptr(grad))
+    return fail(MP_ERR_INVALID_ARG, "grad must be a 16-byte aligned device buffer");
+  if (!out || reinterpret_cast<uintptr_t>(out) % 4 != 0 || !is_device_ptr(out))
+    return fail(MP_ERR_INVALID_ARG, "out must be a 4-byte aligned device buffer");
+  CoefLaunch p;
+  memset(&p, 0, sizeof(p));
+  if ((st = resolve_pointers(family, p.base, p.experts)) != MP_OK) return st;
+  {
+    const char* o0 = reinterpret_cast<const char*>(out);
+    const char* o1 = o0 + (size_t)g.K * g.n_tensors * sizeof(float);
+    auto overlaps = [&](const void* q) {
+      const char* a = static_cast<const char*>(q);
+      return a < o1 && o0 < a + g.span_elems * g.elem_size;
+    };
+    if (overlaps(grad) || overlaps(p.base)) return fail(MP_ERR_INVALID_ARG, "out overlaps grad or the base");
+    for (uint32_t i = 0; i < g.K; ++i)
+      if (overlaps(p.experts.p[i])) return fail(MP_ERR_INVALID_ARG, "out overlaps an expert");
+  }
+  cudaStream_t cs = reinterpret_cast<cudaStream_t>(stream);
+  TraceScope tr(MP_TRACE_COEF, cs);
+  const bool now_captured = capturing(cs);
+  cudaError_t e;
+  if ((e = stream_wait(cs, index->done.get(), index->captured, now_captured)) != cudaSuccess ||
+      (e = stream_wait(cs, plan->done.get(), plan->captured, now_captured)) != cudaSuccess)
+    return cuda_fail(e, "stream wait");
+  p.dtype = g.dtype;
+  p.K = g.K;
+  p.n_tensors = g.n_tensors;
+  p.block_elems = g.max_blk_len;
+  p.n_blocks = g.n_blocks;
+  p.grad = grad;
+  p.blk_off = index->d_blk_off;
+  p.blk_len = index->d_blk_len;
+  p.t_blk0 = index->d_t_blk0;
+  p.mask = plan->d_mask;
+  p.out = out;
+  p.ext = Extents{g.span_elems, g.span_elems};
+  Event done;  // made before the launch, so that what is enqueued has an end to wait for
+  if (!now_captured && (e = done.make()) != cudaSuccess) return cuda_fail(e, "event");
+  Scratch s;
+  if ((e = s.get(coef_scratch(p), cs)) != cudaSuccess) return cuda_fail(e, "scratch");
+  if ((e = launch_coef(p, static_cast<float*>(s.p), cs)) != cudaSuccess) return cuda_fail(e, "coefficient kernels");
+  if (now_captured) return MP_OK;
+  if ((e = cudaEventRecord(done.get(), cs)) != cudaSuccess) return cuda_fail(e, "event record");
+  index->users.add(done);
+  plan->users.add(done);
+  return MP_OK;
+}
+
+mp_status mp_layer_status(mp_stream stream) {
+  const cudaError_t e = cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "stream");
+  uint32_t* w = layer_error_word();
+  const uint32_t err = w ? __atomic_exchange_n(w, 0u, __ATOMIC_ACQ_REL) : 0u;
+  if (err & kErrTimeout) return fail(MP_ERR_TIMEOUT, "a bounded device wait in a linear layer gave up");
+  if (err) return fail(MP_ERR_CUDA, "an internal check of the layer kernels failed");
+  return MP_OK;
 }
 
 mp_status mp_trim(void) {

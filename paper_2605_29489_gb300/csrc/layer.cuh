@@ -1,0 +1,177 @@
+// Internal declarations of the layer operators: norms, linear layers and merge-coefficient
+// gradients (norm.cu, linear.cu, coef.cu behind the entry points of layer_api.cu and api.cu).
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "mp_internal.cuh"
+#include "tma.cuh"
+
+namespace mp {
+
+// ---- from api.cu ------------------------------------------------------------------------------
+// device memory for one call, in stream order from the library's pool; given back in stream order
+cudaError_t scratch_alloc(void** p, size_t bytes, cudaStream_t st);
+void scratch_free(void* p, cudaStream_t st);
+bool device_pointer(const void* p);
+// the pinned host word that kernels of calls without a handle report their errors to (null: no memory)
+uint32_t* layer_error_word();
+uint32_t stall_rounds();  // mp_debug_stall_pipeline
+
+// scratch of one call: given back, in stream order, when the object goes
+struct Scratch {
+  void* p = nullptr;
+  cudaStream_t st = nullptr;
+  Scratch() = default;
+  Scratch(const Scratch&) = delete;
+  Scratch& operator=(const Scratch&) = delete;
+  cudaError_t get(size_t bytes, cudaStream_t s) {
+    st = s;
+    return scratch_alloc(&p, bytes, s);
+  }
+  ~Scratch() {
+    if (p) scratch_free(p, st);
+  }
+};
+
+// ---- element access ----------------------------------------------------------------------------
+template <typename T>
+struct Elem;
+template <>
+struct Elem<float> {
+  static constexpr int kVec = 4;  // elements of a 16-byte access
+  static __device__ __forceinline__ float load(float v) { return v; }
+  static __device__ __forceinline__ float store(float v) { return v; }
+};
+template <>
+struct Elem<__nv_bfloat16> {
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ float load(__nv_bfloat16 v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ __nv_bfloat16 store(float v) { return __float2bfloat16_rn(v); }
+};
+
+// V consecutive elements as they are stored: one 16-byte register group, or a single element
+template <typename T, int V>
+struct alignas(V * sizeof(T)) Pack {
+  T e[V];
+};
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
+  Pack<T, V> r;
+  if constexpr (V * sizeof(T) == 16) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    memcpy(&r, &u, 16);
+  } else {
+    static_assert(V == 1, "whole vectors or single elements");
+    r.e[0] = *p;
+  }
+  return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) {
+  if constexpr (V * sizeof(T) == 16) {
+    uint4 u;
+    memcpy(&u, &v, 16);
+    *reinterpret_cast<uint4*>(p) = u;
+  } else {
+    *p = v.e[0];
+  }
+}
+
+// ---- norm.cu ------------------------------------------------------------------------------------
+struct NormLaunch {
+  mp_dtype dtype;
+  bool layer;  // subtract the mean (layer norm); else RMS norm
+  uint64_t rows;
+  uint32_t cols;
+  float eps;
+  const void *x, *weight, *bias;  // weight and bias may be null
+  uint64_t ldx;
+  void* y;
+  uint64_t ldy;
+  float *mean, *rstd;  // forward: written (may be null); backward: read
+  // backward
+  const void *dy, *add;
+  uint64_t lddy, ldadd, lddx;
+  void *dx, *dweight, *dbias;  // each may be null
+};
+cudaError_t launch_norm(const NormLaunch& p, cudaStream_t st);
+// bytes of scratch that the backward pass needs (0: none)
+size_t norm_backward_scratch(const NormLaunch& p);
+cudaError_t launch_norm_backward(const NormLaunch& p, float* scratch, cudaStream_t st);
+
+// ---- coef.cu ------------------------------------------------------------------------------------
+struct CoefLaunch {
+  mp_dtype dtype;
+  uint32_t K, n_tensors, block_elems;
+  uint64_t n_blocks;
+  const void *base, *grad;
+  ExpertPtrs experts;
+  const uint64_t* blk_off;
+  const uint32_t* blk_len;
+  const uint32_t* t_blk0;
+  const uint32_t* mask;
+  float* out;  // [K][n_tensors]
+  Extents ext;
+};
+size_t coef_scratch(const CoefLaunch& p);
+cudaError_t launch_coef(const CoefLaunch& p, float* scratch, cudaStream_t st);
+
+// ---- linear.cu ----------------------------------------------------------------------------------
+// a matrix in memory: rows x cols elements, element (r, c) at p + r * ld + c
+struct Mat {
+  const void* p = nullptr;
+  uint64_t ld = 0;
+};
+// what follows a product: y = act(acc + bias) * mul + res, pre = acc + bias; every part may be absent.
+// rows x cols is the output's shape, the bias runs along its columns.
+struct Epilogue {
+  uint64_t rows, cols;
+  const void* bias;
+  int act;
+  Mat mul, res;
+  void *y, *pre;
+  uint64_t ldy, ldpre;
+};
+// out[r, c] = sum over k of a(r, k) * b(c, k).  a_t / b_t: the operand is stored with k along its
+// rows (element (r, k) at p + k * ld + r).
+struct GemmLaunch {
+  mp_dtype dtype;
+  Mat a, b;
+  bool a_t, b_t;
+  uint64_t inner;
+  Epilogue e;
+  uint32_t* err;
+  uint32_t wait_limit, stall;
+  bool follows;
+};
+// whether an operand can be read as it is (bf16: 16-byte rows); else it goes through pack()
+bool gemm_operand_ok(mp_dtype dtype, const Mat& m);
+mp_status launch_gemm(const GemmLaunch& g, cudaStream_t st);
+// copies rows x cols elements into dst (row stride ldd)
+cudaError_t launch_repack(mp_dtype dtype, const Mat& m, uint64_t rows, uint64_t cols, void* dst, uint64_t ldd,
+                          cudaStream_t st);
+// the elementwise part of a linear layer's backward pass:
+// dz = dy * mul * act'(pre), dmul = dy * act(pre), db = column sums of dz
+struct DzLaunch {
+  mp_dtype dtype;
+  uint64_t rows, cols;
+  Mat dy, pre, mul;
+  int act;
+  void* dz;  // null where dz is dy itself
+  uint64_t lddz;
+  void* dmul;
+  uint64_t lddmul;
+  void* db;
+};
+size_t dz_scratch(const DzLaunch& p);
+cudaError_t launch_dz(const DzLaunch& p, float* scratch, cudaStream_t st);
+// dst[r, c] = src[r, c], or 0 without a source
+cudaError_t launch_copy_or_zero(mp_dtype dtype, const Mat& src, uint64_t rows, uint64_t cols, void* dst, uint64_t ldd,
+                                cudaStream_t st);
+
+// the sum over n_part rows of part [n_part][cols] into out: the second step of every column sum here
+cudaError_t launch_column_sums(mp_dtype dtype, const float* part, uint32_t n_part, uint32_t cols, void* out,
+                               cudaStream_t st);
+
+}  // namespace mp

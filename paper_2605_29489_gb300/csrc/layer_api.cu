@@ -1,0 +1,387 @@
+// Entry points of the norms and linear layers: argument checks, scratch and the order of the launches.
+#include <math.h>
+
+#include <string>
+
+#include "layer.cuh"
+
+namespace mp {
+
+namespace {
+
+mp_status refuse(const std::string& why) {
+  set_error(why);
+  return MP_ERR_INVALID_ARG;
+}
+
+// no C++ exception leaves an entry point: what the messages and handles allocate may fail
+template <typename F>
+mp_status guarded(F f) {
+  try {
+    return f();
+  } catch (...) {
+    set_static_error("host allocation failed");
+    return MP_ERR_OOM;
+  }
+}
+
+constexpr uint64_t kMaxDim = 0x7FFFFF00ull;  // rows and columns: tile coordinates are 32-bit
+
+// a matrix argument: what it is called, its shape, and whether the call writes it
+struct Arg {
+  const char* name;
+  const void* p;
+  uint64_t ld, rows, cols;
+  bool out;
+};
+
+// pointer, stride and extent of every matrix; outputs lie apart from everything else, or are the very same
+// matrix as the one that `same` names (its index), which the call reads before it writes
+struct Args {
+  uint32_t es;
+  Arg a[16];
+  int same[16];
+  int n = 0;
+  void add(const char* name, const void* p, uint64_t ld, uint64_t rows, uint64_t cols, bool out = false, int may_be = -1) {
+    if (!p) return;
+    a[n] = Arg{name, p, rows <= 1 ? cols : ld, rows, cols, out};
+    same[n++] = may_be;
+  }
+  // index of a matrix added before, or -1
+  int find(const void* p) const {
+    for (int k = 0; k < n; ++k)
+      if (a[k].p == p) return k;
+    return -1;
+  }
+  bool overlap(const Arg& x, const Arg& y) const {
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x.p), y0 = reinterpret_cast<uintptr_t>(y.p);
+    const uint64_t xn = ((x.rows - 1) * x.ld + x.cols) * es, yn = ((y.rows - 1) * y.ld + y.cols) * es;
+    if (x0 + xn <= y0 || y0 + yn <= x0) return false;
+    if (x.ld != y.ld || x.rows <= 1 || y.rows <= 1) return true;
+    // the same row stride: columns of one wider matrix may lie side by side
+    const uint64_t pitch = x.ld * es;
+    const uint64_t d = (y0 >= x0 ? y0 - x0 : pitch - (x0 - y0) % pitch) % pitch;  // y's first column, from x's
+    return !(d >= x.cols * es && d + y.cols * es <= pitch);
+  }
+  mp_status check() const {
+    for (int k = 0; k < n; ++k) {
+      const Arg& x = a[k];
+      if (x.ld < x.cols) return refuse(std::string(x.name) + ": its row stride is smaller than a row");
+      if (x.ld > (1ull << 38) / es) return refuse(std::string(x.name) + ": its row stride is too large");
+      if (reinterpret_cast<uintptr_t>(x.p) % es != 0) return refuse(std::string(x.name) + " is not aligned to its elements");
+      if (!device_pointer(x.p)) return refuse(std::string(x.name) + " must be device memory");
+    }
+    for (int k = 0; k < n; ++k) {
+      if (!a[k].out) continue;
+      for (int q = 0; q < n; ++q) {
+        if (q == k || (a[q].out && q > k)) continue;
+        if (!overlap(a[k], a[q])) continue;
+        if (same[k] == q && a[k].p == a[q].p && a[k].ld == a[q].ld && !a[q].out) continue;
+        return refuse(std::string(a[k].name) + " overlaps " + a[q].name);
+      }
+    }
+    return MP_OK;
+  }
+};
+
+mp_status check_dtype(mp_dtype d) {
+  return d == MP_BF16 || d == MP_F32 ? MP_OK : refuse("dtype must be MP_BF16 or MP_F32");
+}
+
+mp_status check_words(const char* name, const void* p) {
+  if (!p) return MP_OK;
+  if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return refuse(std::string(name) + " is not 4-byte aligned");
+  return device_pointer(p) ? MP_OK : refuse(std::string(name) + " must be device memory");
+}
+
+mp_status norm_shape(mp_dtype dtype, mp_norm_kind kind, uint64_t rows, uint64_t cols) {
+  mp_status st;
+  if ((st = check_dtype(dtype)) != MP_OK) return st;
+  if (kind != MP_NORM_RMS && kind != MP_NORM_LAYER) return refuse("unknown norm kind");
+  if (cols < 1 || cols > (1u << 28)) return refuse("cols must be in [1, 2^28]");
+  if (rows > (1ull << 48)) return refuse("too many rows");
+  return MP_OK;
+}
+
+cudaStream_t stream_of(mp_stream s) { return reinterpret_cast<cudaStream_t>(s); }
+
+// an operand that the tensor cores can read: itself, or a copy with rows of whole 16-byte vectors
+mp_status readable(mp_dtype dtype, Mat& m, uint64_t rows, uint64_t cols, Scratch& s, cudaStream_t cs) {
+  if (rows <= 1) m.ld = (cols + 7) / 8 * 8;  // no second row: any stride will do
+  if (gemm_operand_ok(dtype, m)) return MP_OK;
+  const uint64_t ld = (cols + 7) / 8 * 8;
+  cudaError_t e;
+  if ((e = s.get(rows * ld * 2, cs)) != cudaSuccess) return cuda_fail(e, "scratch");
+  if ((e = launch_repack(dtype, m, rows, cols, s.p, ld, cs)) != cudaSuccess) return cuda_fail(e, "copy kernel");
+  m = Mat{s.p, ld};
+  return MP_OK;
+}
+
+mp_status linear_shape(mp_dtype dtype, mp_act act, uint64_t rows, uint64_t in, uint64_t out) {
+  mp_status st;
+  if ((st = check_dtype(dtype)) != MP_OK) return st;
+  if (act < MP_ACT_NONE || act > MP_ACT_GELU_TANH) return refuse("unknown activation");
+  if (in < 1 || out < 1 || in > kMaxDim || out > kMaxDim) return refuse("in and out must be in [1, 2^31 - 256]");
+  if (rows > kMaxDim) return refuse("too many rows");
+  return MP_OK;
+}
+
+mp_status error_word(GemmLaunch& g) {
+  g.err = layer_error_word();
+  if (!g.err) {
+    set_static_error("pinned host allocation failed");
+    return MP_ERR_OOM;
+  }
+  g.wait_limit = stall_rounds();
+  g.stall = g.wait_limit ? 1u : 0u;
+  return MP_OK;
+}
+
+mp_status norm(const mp_norm_args& a, mp_stream stream) {
+  mp_status st;
+  if ((st = norm_shape(a.dtype, a.kind, a.rows, a.cols)) != MP_OK) return st;
+  if (!(a.eps >= 0.0f) || isinf(a.eps)) return refuse("eps must be finite and not negative");
+  if (a.kind == MP_NORM_RMS && (a.bias || a.mean)) return refuse("an RMS norm has no bias and no mean");
+  if (a.rows == 0) return MP_OK;
+  if (!a.x.data || !a.y.data) return refuse("x or y is NULL");
+  Args c;
+  c.es = a.dtype == MP_BF16 ? 2 : 4;
+  c.add("x", a.x.data, a.x.ld, a.rows, a.cols);
+  c.add("weight", a.weight, a.cols, 1, a.cols);
+  c.add("bias", a.bias, a.cols, 1, a.cols);
+  c.add("y", a.y.data, a.y.ld, a.rows, a.cols, true, 0);
+  if ((st = c.check()) != MP_OK) return st;
+  if ((st = check_words("mean", a.mean)) != MP_OK || (st = check_words("rstd", a.rstd)) != MP_OK) return st;
+  NormLaunch p = {};
+  p.dtype = a.dtype;
+  p.layer = a.kind == MP_NORM_LAYER;
+  p.rows = a.rows;
+  p.cols = (uint32_t)a.cols;
+  p.eps = a.eps;
+  p.x = a.x.data;
+  p.ldx = a.x.ld;
+  p.weight = a.weight;
+  p.bias = a.bias;
+  p.y = a.y.data;
+  p.ldy = a.y.ld;
+  p.mean = a.mean;
+  p.rstd = a.rstd;
+  TraceScope tr(MP_TRACE_NORM, stream_of(stream));
+  const cudaError_t e = launch_norm(p, stream_of(stream));
+  return e == cudaSuccess ? MP_OK : cuda_fail(e, "norm kernel");
+}
+
+mp_status norm_backward(const mp_norm_backward_args& a, mp_stream stream) {
+  mp_status st;
+  if ((st = norm_shape(a.dtype, a.kind, a.rows, a.cols)) != MP_OK) return st;
+  if (a.kind == MP_NORM_RMS && (a.mean || a.dbias)) return refuse("an RMS norm has no bias and no mean");
+  if (a.dweight && !a.weight) return refuse("dweight is given, weight is not");
+  if (a.add.data && !a.dx.data) return refuse("add is given, dx is not");
+  if (!a.dx.data && !a.dweight && !a.dbias) return MP_OK;
+  cudaStream_t cs = stream_of(stream);
+  Args c;
+  c.es = a.dtype == MP_BF16 ? 2 : 4;
+  cudaError_t e;
+  if (a.rows > 0) {
+    if (!a.dy.data || !a.x.data || !a.rstd) return refuse("dy, x or rstd is NULL");
+    if (a.kind == MP_NORM_LAYER && !a.mean) return refuse("mean is NULL");
+    c.add("dy", a.dy.data, a.dy.ld, a.rows, a.cols);
+    c.add("x", a.x.data, a.x.ld, a.rows, a.cols);
+    c.add("add", a.add.data, a.add.ld, a.rows, a.cols);
+    c.add("weight", a.weight, a.cols, 1, a.cols);
+    c.add("dx", a.dx.data, a.dx.ld, a.rows, a.cols, true, a.add.data ? c.find(a.add.data) : -1);
+  }
+  c.add("dweight", a.dweight, a.cols, 1, a.cols, true);
+  c.add("dbias", a.dbias, a.cols, 1, a.cols, true);
+  if ((st = c.check()) != MP_OK) return st;
+  if ((st = check_words("mean", a.mean)) != MP_OK || (st = check_words("rstd", a.rstd)) != MP_OK) return st;
+  TraceScope tr(MP_TRACE_NORM, cs);
+  if (a.rows == 0) {  // sums over no rows
+    for (void* d : {a.dweight, a.dbias})
+      if (d && (e = launch_copy_or_zero(a.dtype, Mat{}, 1, a.cols, d, a.cols, cs)) != cudaSuccess)
+        return cuda_fail(e, "fill kernel");
+    return MP_OK;
+  }
+  NormLaunch p = {};
+  p.dtype = a.dtype;
+  p.layer = a.kind == MP_NORM_LAYER;
+  p.rows = a.rows;
+  p.cols = (uint32_t)a.cols;
+  p.dy = a.dy.data;
+  p.lddy = a.dy.ld;
+  p.x = a.x.data;
+  p.ldx = a.x.ld;
+  p.weight = a.weight;
+  p.mean = const_cast<float*>(a.mean);  // read by the backward pass
+  p.rstd = const_cast<float*>(a.rstd);
+  p.add = a.add.data;
+  p.ldadd = a.add.ld;
+  p.dx = a.dx.data;
+  p.lddx = a.dx.ld;
+  p.dweight = a.dweight;
+  p.dbias = a.dbias;
+  Scratch s;
+  if (const size_t bytes = norm_backward_scratch(p))
+    if ((e = s.get(bytes, cs)) != cudaSuccess) return cuda_fail(e, "scratch");
+  e = launch_norm_backward(p, static_cast<float*>(s.p), cs);
+  return e == cudaSuccess ? MP_OK : cuda_fail(e, "norm kernel");
+}
+
+mp_status linear(const mp_linear_args& a, mp_stream stream) {
+  mp_status st;
+  if ((st = linear_shape(a.dtype, a.act, a.rows, a.in, a.out)) != MP_OK) return st;
+  if (a.rows == 0) return MP_OK;
+  if (!a.x.data || !a.w.data || !a.y.data) return refuse("x, w or y is NULL");
+  Args c;
+  c.es = a.dtype == MP_BF16 ? 2 : 4;
+  c.add("x", a.x.data, a.x.ld, a.rows, a.in);
+  c.add("w", a.w.data, a.w.ld, a.out, a.in);
+  c.add("bias", a.bias, a.out, 1, a.out);
+  c.add("mul", a.mul.data, a.mul.ld, a.rows, a.out);
+  c.add("residual", a.residual.data, a.residual.ld, a.rows, a.out);
+  // y may be the factor or the residual: an element's are read before it is written, by the same thread
+  int may = a.residual.data == a.y.data ? c.find(a.residual.data) : -1;
+  if (may < 0 && a.mul.data == a.y.data) may = c.find(a.mul.data);
+  c.add("y", a.y.data, a.y.ld, a.rows, a.out, true, may);
+  c.add("pre", a.pre.data, a.pre.ld, a.rows, a.out, true);
+  if ((st = c.check()) != MP_OK) return st;
+  cudaStream_t cs = stream_of(stream);
+  TraceScope tr(MP_TRACE_LINEAR, cs);
+  GemmLaunch g = {};
+  if ((st = error_word(g)) != MP_OK) return st;
+  Scratch sx, sw;
+  g.dtype = a.dtype;
+  g.a = Mat{a.x.data, a.x.ld};
+  g.b = Mat{a.w.data, a.w.ld};
+  if ((st = readable(a.dtype, g.a, a.rows, a.in, sx, cs)) != MP_OK) return st;
+  if ((st = readable(a.dtype, g.b, a.out, a.in, sw, cs)) != MP_OK) return st;
+  g.follows = sx.p || sw.p;
+  g.inner = a.in;
+  g.e = Epilogue{a.rows, a.out, a.bias, a.act, Mat{a.mul.data, a.mul.ld}, Mat{a.residual.data, a.residual.ld},
+                 a.y.data, a.pre.data, a.y.ld, a.pre.ld};
+  return launch_gemm(g, cs);
+}
+
+mp_status linear_backward(const mp_linear_backward_args& a, mp_stream stream) {
+  mp_status st;
+  if ((st = linear_shape(a.dtype, a.act, a.rows, a.in, a.out)) != MP_OK) return st;
+  if (a.dmul.data && !a.mul.data) return refuse("dmul is given, mul is not");
+  if (a.dx_add.data && !a.dx.data) return refuse("dx_add is given, dx is not");
+  if (a.dw_add.data && !a.dw.data) return refuse("dw_add is given, dw is not");
+  if (a.rows > 0 && !a.pre.data && (a.act != MP_ACT_NONE || a.dmul.data)) return refuse("pre is needed for act and for dmul");
+  if (!a.dx.data && !a.dw.data && !a.db && !a.dmul.data) return MP_OK;
+  if (a.rows > 0) {
+    if (!a.dy.data) return refuse("dy is NULL");
+    if (a.dx.data && !a.w.data) return refuse("w is needed for dx");
+    if (a.dw.data && !a.x.data) return refuse("x is needed for dw");
+  }
+  cudaStream_t cs = stream_of(stream);
+  const uint32_t es = a.dtype == MP_BF16 ? 2 : 4;
+  Args c;
+  c.es = es;
+  if (a.rows > 0) {
+    c.add("dy", a.dy.data, a.dy.ld, a.rows, a.out);
+    if (a.dw.data) c.add("x", a.x.data, a.x.ld, a.rows, a.in);
+    if (a.dx.data) c.add("w", a.w.data, a.w.ld, a.out, a.in);
+    c.add("pre", a.pre.data, a.pre.ld, a.rows, a.out);
+    c.add("mul", a.mul.data, a.mul.ld, a.rows, a.out);
+    c.add("dx_add", a.dx_add.data, a.dx_add.ld, a.rows, a.in);
+    c.add("dx", a.dx.data, a.dx.ld, a.rows, a.in, true, a.dx_add.data ? c.find(a.dx_add.data) : -1);
+    c.add("dmul", a.dmul.data, a.dmul.ld, a.rows, a.out, true);
+  }
+  c.add("dw_add", a.dw_add.data, a.dw_add.ld, a.out, a.in);
+  c.add("dw", a.dw.data, a.dw.ld, a.out, a.in, true, a.dw_add.data ? c.find(a.dw_add.data) : -1);
+  c.add("db", a.db, a.out, 1, a.out, true);
+  if ((st = c.check()) != MP_OK) return st;
+  TraceScope tr(MP_TRACE_LINEAR, cs);
+  cudaError_t e;
+  if (a.rows == 0) {  // sums over no rows
+    if (a.dw.data && !(a.dw_add.data == a.dw.data) &&
+        (e = launch_copy_or_zero(a.dtype, Mat{a.dw_add.data, a.dw_add.ld}, a.out, a.in, a.dw.data, a.dw.ld, cs)) != cudaSuccess)
+      return cuda_fail(e, "fill kernel");
+    if (a.db && (e = launch_copy_or_zero(a.dtype, Mat{}, 1, a.out, a.db, a.out, cs)) != cudaSuccess)
+      return cuda_fail(e, "fill kernel");
+    return MP_OK;
+  }
+  GemmLaunch g = {};
+  if ((st = error_word(g)) != MP_OK) return st;
+  g.dtype = a.dtype;
+  Scratch sz, sp, sx, sw;
+  Mat dz{a.dy.data, a.dy.ld};
+  const bool products = a.dx.data || a.dw.data;
+  const bool changed = a.act != MP_ACT_NONE || a.mul.data;
+  if (a.rows == 1) dz.ld = (a.out + 7) / 8 * 8;
+  const bool own_dz = products && (changed || !gemm_operand_ok(a.dtype, dz));
+  if (own_dz || a.db || a.dmul.data) {
+    DzLaunch d = {};
+    d.dtype = a.dtype;
+    d.rows = a.rows;
+    d.cols = a.out;
+    d.dy = Mat{a.dy.data, a.dy.ld};
+    d.pre = Mat{a.pre.data, a.pre.ld};
+    d.mul = Mat{a.mul.data, a.mul.ld};
+    d.act = a.act;
+    d.dmul = a.dmul.data;
+    d.lddmul = a.dmul.ld;
+    d.db = a.db;
+    if (own_dz) {
+      d.lddz = (a.out + 7) / 8 * 8;
+      if ((e = sz.get(a.rows * d.lddz * es, cs)) != cudaSuccess) return cuda_fail(e, "scratch");
+      d.dz = sz.p;
+      dz = Mat{sz.p, d.lddz};
+    }
+    if (const size_t bytes = dz_scratch(d))
+      if ((e = sp.get(bytes, cs)) != cudaSuccess) return cuda_fail(e, "scratch");
+    if ((e = launch_dz(d, static_cast<float*>(sp.p), cs)) != cudaSuccess) return cuda_fail(e, "linear kernel");
+    g.follows = true;
+  }
+  if (a.dx.data) {
+    g.a = dz;
+    g.b = Mat{a.w.data, a.w.ld};
+    if ((st = readable(a.dtype, g.b, a.out, a.in, sw, cs)) != MP_OK) return st;
+    g.a_t = false;
+    g.b_t = true;
+    g.inner = a.out;
+    g.e = Epilogue{a.rows, a.in, nullptr, MP_ACT_NONE, Mat{}, Mat{a.dx_add.data, a.dx_add.ld}, a.dx.data, nullptr, a.dx.ld, 0};
+    g.follows = g.follows || sw.p;
+    if ((st = launch_gemm(g, cs)) != MP_OK) return st;
+    g.follows = true;
+  }
+  if (a.dw.data) {
+    g.a = dz;
+    g.b = Mat{a.x.data, a.x.ld};
+    if ((st = readable(a.dtype, g.b, a.rows, a.in, sx, cs)) != MP_OK) return st;
+    g.a_t = g.b_t = true;
+    g.inner = a.rows;
+    g.e = Epilogue{a.out, a.in, nullptr, MP_ACT_NONE, Mat{}, Mat{a.dw_add.data, a.dw_add.ld}, a.dw.data, nullptr, a.dw.ld, 0};
+    g.follows = g.follows || sx.p;
+    if ((st = launch_gemm(g, cs)) != MP_OK) return st;
+  }
+  return MP_OK;
+}
+
+template <typename A>
+mp_status entry(const char* name, mp_status (*f)(const A&, mp_stream), const A* args, mp_stream stream) {
+  NvtxScope nv(name);
+  return guarded([&] { return args ? f(*args, stream) : refuse("args is NULL"); });
+}
+
+}  // namespace
+
+}  // namespace mp
+
+extern "C" {
+
+mp_status mp_norm(const mp_norm_args* args, mp_stream stream) { return mp::entry("mp_norm", mp::norm, args, stream); }
+
+mp_status mp_norm_backward(const mp_norm_backward_args* args, mp_stream stream) {
+  return mp::entry("mp_norm_backward", mp::norm_backward, args, stream);
+}
+
+mp_status mp_linear(const mp_linear_args* args, mp_stream stream) { return mp::entry("mp_linear", mp::linear, args, stream); }
+
+mp_status mp_linear_backward(const mp_linear_backward_args* args, mp_stream stream) {
+  return mp::entry("mp_linear_backward", mp::linear_backward, args, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,534 @@
+// Layer norm and RMS norm of the rows of a matrix, forward and backward.
+//
+//   mu = mean(x) (layer norm; 0 for RMS norm),  v = mean((x - mu)^2),  rstd = 1 / sqrt(v + eps)
+//   xh = (x - mu) * rstd,  y = xh * w + b
+//   g = dy * w,  dx = rstd * (g - mean(g) [layer norm] - xh * mean(g * xh)) + add
+//   dw = sum over rows of dy * xh,  db = sum over rows of dy
+//
+// Bound by memory: a row is read once into registers, and the variance is that of the centred values
+// (two reductions for layer norm, one for RMS norm), not a difference of large sums.  Statistics,
+// products and the weights' gradients are fp32; each output is rounded once.
+//
+// The backward pass adds up dw and db in registers over the rows of a CTA, a thread holding the same
+// columns for each of them; the CTAs' sums go to scratch, and a second kernel adds those in a fixed
+// order, so that a result does not depend on what ran when.
+#include <algorithm>
+
+#include "layer.cuh"
+
+namespace mp {
+
+namespace {
+
+constexpr uint32_t kWideCols = 8192;    // the widest row of the backward pass with sums in registers
+constexpr uint32_t kNormCols = 16384;   // the widest row of the forward pass in registers
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  return v;
+}
+
+// sums of two values over the ROWT threads of a row; red: 2 floats per warp of the CTA.  Every thread gets the same
+// bits: with more than one warp each adds the warps' sums in the same order.
+template <int ROWT>
+__device__ __forceinline__ float2 row_sum2(float a, float b, float2* red) {
+  a = warp_sum(a);
+  b = warp_sum(b);
+  if constexpr (ROWT > 32) {
+    constexpr int W = ROWT / 32;
+    const int warp = threadIdx.x >> 5, first = (threadIdx.x / ROWT) * W;
+    if ((threadIdx.x & 31) == 0) red[warp] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      a += red[first + w].x;
+      b += red[first + w].y;
+    }
+    __syncthreads();
+  }
+  return make_float2(a, b);
+}
+
+// threads of a CTA for rows of ROWT threads: at least four warps
+template <int ROWT>
+constexpr int cta_of() {
+  return ROWT < 128 ? 128 : ROWT;
+}
+
+template <typename T, int V, int NV, int ROWT, bool LAYER>
+__global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_kernel(const NormLaunch p) {
+  kernel_begin();
+  constexpr int kRows = cta_of<ROWT>() / ROWT;
+  __shared__ float2 red[cta_of<ROWT>() / 32];
+  const int lane = threadIdx.x % ROWT;
+  const T* w = static_cast<const T*>(p.weight);
+  const T* b = static_cast<const T*>(p.bias);
+  const float inv = 1.0f / (float)p.cols;
+  // the rows of a CTA go on together (its threads meet at the sums): r0 is the same for all of them
+  for (uint64_t r0 = (uint64_t)blockIdx.x * kRows; r0 < p.rows; r0 += (uint64_t)gridDim.x * kRows) {
+    const uint64_t r = r0 + threadIdx.x / ROWT;
+    const bool live = r < p.rows;
+    const T* x = static_cast<const T*>(p.x) + (live ? r : r0) * p.ldx;
+    float v[NV * V];
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+      Pack<T, V> q;
+      if (c < p.cols) q = load_pack<T, V>(x + c);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        v[k * V + e] = c < p.cols ? Elem<T>::load(q.e[e]) : 0.0f;
+        s = LAYER ? s + v[k * V + e] : fmaf(v[k * V + e], v[k * V + e], s);
+      }
+    }
+    float mu = 0.0f;
+    if (LAYER) {
+      mu = row_sum2<ROWT>(s, 0.0f, red).x * inv;
+      s = 0.0f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          v[k * V + e] -= mu;
+          if (c < p.cols) s = fmaf(v[k * V + e], v[k * V + e], s);
+        }
+      }
+    }
+    const float var = row_sum2<ROWT>(s, 0.0f, red).x * inv;
+    const float rstd = 1.0f / sqrtf(var + p.eps);
+    if (live) {
+      if (lane == 0) {
+        if (p.rstd) p.rstd[r] = rstd;
+        if (LAYER && p.mean) p.mean[r] = mu;
+      }
+      T* y = static_cast<T*>(p.y) + r * p.ldy;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+        if (c < p.cols) {
+          Pack<T, V> o, wq, bq;
+          if (w) wq = load_pack<T, V>(w + c);
+          if (b) bq = load_pack<T, V>(b + c);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            float t = v[k * V + e] * rstd;
+            if (w) t *= Elem<T>::load(wq.e[e]);
+            if (b) t += Elem<T>::load(bq.e[e]);
+            o.e[e] = Elem<T>::store(t);
+          }
+          store_pack<T, V>(y + c, o);
+        }
+      }
+    }
+  }
+}
+
+// rows wider than the registers of a CTA hold: read again for each step (from L2)
+template <typename T, int V, bool LAYER>
+__global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) {
+  kernel_begin();
+  __shared__ float2 red[32];
+  const T* w = static_cast<const T*>(p.weight);
+  const T* b = static_cast<const T*>(p.bias);
+  const float inv = 1.0f / (float)p.cols;
+  for (uint64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+    const T* x = static_cast<const T*>(p.x) + r * p.ldx;
+    float mu = 0.0f, s = 0.0f;
+    if (LAYER) {
+      for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
+        const Pack<T, V> q = load_pack<T, V>(x + c);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += Elem<T>::load(q.e[e]);
+      }
+      mu = row_sum2<1024>(s, 0.0f, red).x * inv;
+      s = 0.0f;
+    }
+    for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
+      const Pack<T, V> q = load_pack<T, V>(x + c);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float t = Elem<T>::load(q.e[e]) - mu;
+        s = fmaf(t, t, s);
+      }
+    }
+    const float rstd = 1.0f / sqrtf(row_sum2<1024>(s, 0.0f, red).x * inv + p.eps);
+    if (threadIdx.x == 0) {
+      if (p.rstd) p.rstd[r] = rstd;
+      if (LAYER && p.mean) p.mean[r] = mu;
+    }
+    T* y = static_cast<T*>(p.y) + r * p.ldy;
+    for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
+      const Pack<T, V> q = load_pack<T, V>(x + c);
+      Pack<T, V> o, wq, bq;
+      if (w) wq = load_pack<T, V>(w + c);
+      if (b) bq = load_pack<T, V>(b + c);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float t = (Elem<T>::load(q.e[e]) - mu) * rstd;
+        if (w) t *= Elem<T>::load(wq.e[e]);
+        if (b) t += Elem<T>::load(bq.e[e]);
+        o.e[e] = Elem<T>::store(t);
+      }
+      store_pack<T, V>(y + c, o);
+    }
+  }
+}
+
+// dx of the rows of a CTA and its sums for dw (part [2 * cta]) and db (part [2 * cta + 1]); sums: whether those
+// are wanted.  NV * V is 16 at most: x and dy stay as they are stored, the sums take two registers a column.
+template <typename T, int V, int NV, int ROWT, bool LAYER>
+__global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_backward_kernel(const NormLaunch p, float* part) {
+  kernel_begin();
+  constexpr int kRows = cta_of<ROWT>() / ROWT;
+  __shared__ float2 red[cta_of<ROWT>() / 32];
+  const int lane = threadIdx.x % ROWT;
+  const T* w = static_cast<const T*>(p.weight);
+  const float inv = 1.0f / (float)p.cols;
+  float aw[NV * V] = {}, ab[NV * V] = {};
+  for (uint64_t r0 = (uint64_t)blockIdx.x * kRows; r0 < p.rows; r0 += (uint64_t)gridDim.x * kRows) {
+    const uint64_t r = r0 + threadIdx.x / ROWT;
+    const bool live = r < p.rows;
+    const uint64_t rr = live ? r : r0;
+    const T* x = static_cast<const T*>(p.x) + rr * p.ldx;
+    const T* dy = static_cast<const T*>(p.dy) + rr * p.lddy;
+    const float mu = LAYER ? p.mean[rr] : 0.0f, rstd = p.rstd[rr];
+    Pack<T, V> xq[NV], dq[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+      if (c < p.cols) {
+        xq[k] = load_pack<T, V>(x + c);
+        dq[k] = load_pack<T, V>(dy + c);
+      }
+    }
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+      if (c < p.cols) {
+        Pack<T, V> wq;
+        if (w) wq = load_pack<T, V>(w + c);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float d = Elem<T>::load(dq[k].e[e]);
+          const float h = (Elem<T>::load(xq[k].e[e]) - mu) * rstd;
+          const float g = w ? d * Elem<T>::load(wq.e[e]) : d;
+          s1 = fmaf(g, h, s1);
+          if (LAYER) s2 += g;
+          if (live) {
+            aw[k * V + e] = fmaf(d, h, aw[k * V + e]);
+            if (LAYER) ab[k * V + e] += d;
+          }
+        }
+      }
+    }
+    if (!p.dx) continue;
+    const float2 m = row_sum2<ROWT>(s1, s2, red);
+    const float m1 = m.x * inv, m2 = m.y * inv;
+    if (live) {
+      T* dx = static_cast<T*>(p.dx) + r * p.lddx;
+      const T* add = p.add ? static_cast<const T*>(p.add) + r * p.ldadd : nullptr;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+        if (c < p.cols) {
+          Pack<T, V> o, wq, aq;
+          if (w) wq = load_pack<T, V>(w + c);
+          if (add) aq = load_pack<T, V>(add + c);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float d = Elem<T>::load(dq[k].e[e]);
+            const float h = (Elem<T>::load(xq[k].e[e]) - mu) * rstd;
+            float t = w ? d * Elem<T>::load(wq.e[e]) : d;
+            if (LAYER) t -= m2;
+            t = (t - h * m1) * rstd;
+            if (add) t += Elem<T>::load(aq.e[e]);
+            o.e[e] = Elem<T>::store(t);
+          }
+          store_pack<T, V>(dx + c, o);
+        }
+      }
+    }
+  }
+  if (!part) return;
+  // rows that share a CTA: their sums are added in the order of the rows, through shared memory
+  float* pw = part + (uint64_t)blockIdx.x * 2 * p.cols;
+  float* pb = pw + p.cols;
+  if constexpr (kRows > 1) {
+    __shared__ float add_up[kRows][ROWT * NV * V];
+#pragma unroll
+    for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          add_up[threadIdx.x / ROWT][(k * ROWT + lane) * V + e] = which ? ab[k * V + e] : aw[k * V + e];
+      __syncthreads();
+      for (uint32_t c = threadIdx.x; c < p.cols; c += blockDim.x) {
+        float s = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kRows; ++q) s += add_up[q][c];
+        (which ? pb : pw)[c] = s;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+      if (c < p.cols) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          pw[c + e] = aw[k * V + e];
+          if (LAYER) pb[c + e] = ab[k * V + e];
+        }
+      }
+    }
+  }
+}
+
+// wide rows: dx alone, x and dy read twice
+template <typename T, int V, bool LAYER>
+__global__ void __launch_bounds__(1024, 1) norm_backward_wide_kernel(const NormLaunch p) {
+  kernel_begin();
+  __shared__ float2 red[32];
+  const T* w = static_cast<const T*>(p.weight);
+  const float inv = 1.0f / (float)p.cols;
+  for (uint64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+    const T* x = static_cast<const T*>(p.x) + r * p.ldx;
+    const T* dy = static_cast<const T*>(p.dy) + r * p.lddy;
+    const T* add = p.add ? static_cast<const T*>(p.add) + r * p.ldadd : nullptr;
+    const float mu = LAYER ? p.mean[r] : 0.0f, rstd = p.rstd[r];
+    float s1 = 0.0f, s2 = 0.0f;
+    for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
+      const Pack<T, V> xq = load_pack<T, V>(x + c), dq = load_pack<T, V>(dy + c);
+      Pack<T, V> wq;
+      if (w) wq = load_pack<T, V>(w + c);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = Elem<T>::load(dq.e[e]);
+        const float g = w ? d * Elem<T>::load(wq.e[e]) : d;
+        s1 = fmaf(g, (Elem<T>::load(xq.e[e]) - mu) * rstd, s1);
+        s2 += g;
+      }
+    }
+    const float2 m = row_sum2<1024>(s1, s2, red);
+    const float m1 = m.x * inv, m2 = LAYER ? m.y * inv : 0.0f;
+    T* dx = static_cast<T*>(p.dx) + r * p.lddx;
+    for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
+      const Pack<T, V> xq = load_pack<T, V>(x + c), dq = load_pack<T, V>(dy + c);
+      Pack<T, V> wq, aq, o;
+      if (w) wq = load_pack<T, V>(w + c);
+      if (add) aq = load_pack<T, V>(add + c);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = Elem<T>::load(dq.e[e]);
+        const float g = w ? d * Elem<T>::load(wq.e[e]) : d;
+        const float h = (Elem<T>::load(xq.e[e]) - mu) * rstd;
+        float t = (g - m2 - h * m1) * rstd;
+        if (add) t += Elem<T>::load(aq.e[e]);
+        o.e[e] = Elem<T>::store(t);
+      }
+      store_pack<T, V>(dx + c, o);
+    }
+  }
+}
+
+// wide rows: the sums for dw and db, 256 columns and a run of rows to a CTA
+template <typename T, bool LAYER>
+__global__ void __launch_bounds__(256) norm_weight_sums_kernel(const NormLaunch p, float* part, uint64_t rows_each) {
+  kernel_begin();
+  const uint32_t c = blockIdx.x * 256u + threadIdx.x;
+  const uint64_t r0 = blockIdx.y * rows_each, r1 = r0 + rows_each < p.rows ? r0 + rows_each : p.rows;
+  if (c >= p.cols) return;
+  float aw = 0.0f, ab = 0.0f;
+  for (uint64_t r = r0; r < r1; ++r) {
+    const float d = Elem<T>::load(static_cast<const T*>(p.dy)[r * p.lddy + c]);
+    const float x = Elem<T>::load(static_cast<const T*>(p.x)[r * p.ldx + c]);
+    aw = fmaf(d, (LAYER ? x - p.mean[r] : x) * p.rstd[r], aw);
+    ab += d;
+  }
+  part[(uint64_t)blockIdx.y * 2 * p.cols + c] = aw;
+  part[((uint64_t)blockIdx.y * 2 + 1) * p.cols + c] = ab;
+}
+
+// out[c] = sum over q of part[q * stride + c], 32 columns to a CTA: eight warps take every eighth part each, then
+// their sums are added in order
+template <typename T>
+__global__ void __launch_bounds__(256) column_sums_kernel(const float* part, uint32_t n_part, uint64_t stride,
+                                                          uint32_t cols, T* out, T* out2) {
+  kernel_begin();
+  __shared__ float s[8][33];
+  const uint32_t c = blockIdx.x * 32u + (threadIdx.x & 31u), w = threadIdx.x >> 5;
+  const float* src = part + (blockIdx.y ? cols : 0u);
+  T* dst = blockIdx.y ? out2 : out;
+  float a0 = 0.0f, a1 = 0.0f, a2 = 0.0f, a3 = 0.0f;
+  if (c < cols && dst) {
+    uint32_t q = w;
+    for (; q + 24u < n_part; q += 32u) {
+      a0 += src[q * stride + c];
+      a1 += src[(q + 8u) * stride + c];
+      a2 += src[(q + 16u) * stride + c];
+      a3 += src[(q + 24u) * stride + c];
+    }
+    for (; q < n_part; q += 8u) a0 += src[q * stride + c];
+  }
+  s[w][threadIdx.x & 31u] = (a0 + a1) + (a2 + a3);
+  __syncthreads();
+  if (w == 0 && c < cols && dst) {
+    float t = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t += s[k][threadIdx.x];
+    dst[c] = Elem<T>::store(t);
+  }
+}
+
+bool aligned16(const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15u) == 0; }
+bool row16(const void* q, uint64_t ld, size_t es) { return !q || (aligned16(q) && (ld * es) % 16 == 0); }
+
+// whole 16-byte vectors where every row of every matrix allows them
+bool vectors_ok(const NormLaunch& p, bool backward) {
+  const size_t es = p.dtype == MP_BF16 ? 2 : 4;
+  if ((p.cols * es) % 16 != 0 || !row16(p.x, p.ldx, es) || !row16(p.weight, 0, es)) return false;
+  if (!backward) return row16(p.y, p.ldy, es) && row16(p.bias, 0, es);
+  return row16(p.dy, p.lddy, es) && row16(p.add, p.ldadd, es) && row16(p.dx, p.lddx, es);
+}
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return 152;
+  }
+  return n;
+}
+
+// threads per row: the vectors of a row over NV per thread
+template <int V, int NV>
+int threads_for(uint32_t cols) {
+  const uint32_t need = (cols + V * NV - 1) / (V * NV);
+  return need <= 32 ? 32 : need <= 128 ? 128 : need <= 256 ? 256 : need <= 512 ? 512 : 1024;
+}
+
+template <typename T, int V, int NV, bool LAYER>
+cudaError_t norm_forward(const NormLaunch& p, cudaStream_t st) {
+  const int t = threads_for<V, NV>(p.cols);
+  const uint64_t ctas = t == 32 ? (p.rows + 3) / 4 : p.rows;
+  const uint64_t most = (uint64_t)sm_count() * (2048 / std::max(t, 128));
+  const dim3 grid((unsigned)std::min(ctas, most));
+  switch (t) {
+    case 32: return launch_kernel(false, norm_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p);
+    case 128: return launch_kernel(false, norm_kernel<T, V, NV, 128, LAYER>, grid, 128, 0, st, p);
+    case 256: return launch_kernel(false, norm_kernel<T, V, NV, 256, LAYER>, grid, 256, 0, st, p);
+    case 512: return launch_kernel(false, norm_kernel<T, V, NV, 512, LAYER>, grid, 512, 0, st, p);
+    default: return launch_kernel(false, norm_kernel<T, V, NV, 1024, LAYER>, grid, 1024, 0, st, p);
+  }
+}
+
+template <typename T, bool LAYER>
+cudaError_t norm_forward_of(const NormLaunch& p, cudaStream_t st) {
+  constexpr int V = Elem<T>::kVec;
+  const bool vec = vectors_ok(p, false);
+  if (p.cols > kNormCols) {
+    const dim3 grid((unsigned)std::min<uint64_t>(p.rows, (uint64_t)sm_count() * 2));
+    return vec ? launch_kernel(false, norm_wide_kernel<T, V, LAYER>, grid, 1024, 0, st, p)
+               : launch_kernel(false, norm_wide_kernel<T, 1, LAYER>, grid, 1024, 0, st, p);
+  }
+  return vec ? norm_forward<T, V, 16 / V, LAYER>(p, st) : norm_forward<T, 1, 16, LAYER>(p, st);
+}
+
+// the CTAs of the backward pass: sums of fewer CTAs are less to write and read again
+template <int V, int NV>
+uint32_t backward_ctas(const NormLaunch& p) {
+  const int t = threads_for<V, NV>(p.cols);
+  const uint64_t ctas = t == 32 ? (p.rows + 3) / 4 : p.rows;
+  return (uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * (t >= 512 ? 1 : t == 256 ? 2 : 4));
+}
+
+constexpr uint32_t kWideParts = 64;
+
+uint32_t backward_parts(const NormLaunch& p) {
+  if (p.cols > kWideCols) return (uint32_t)std::min<uint64_t>(kWideParts, p.rows);
+  const bool vec = vectors_ok(p, true);
+  if (!vec) return backward_ctas<1, 16>(p);
+  return p.dtype == MP_BF16 ? backward_ctas<8, 2>(p) : backward_ctas<4, 4>(p);
+}
+
+template <typename T, int V, int NV, bool LAYER>
+cudaError_t norm_backward(const NormLaunch& p, float* part, cudaStream_t st) {
+  const int t = threads_for<V, NV>(p.cols);
+  const dim3 grid(backward_ctas<V, NV>(p));
+  switch (t) {
+    case 32: return launch_kernel(false, norm_backward_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p, part);
+    case 128: return launch_kernel(false, norm_backward_kernel<T, V, NV, 128, LAYER>, grid, 128, 0, st, p, part);
+    case 256: return launch_kernel(false, norm_backward_kernel<T, V, NV, 256, LAYER>, grid, 256, 0, st, p, part);
+    default: return launch_kernel(false, norm_backward_kernel<T, V, NV, 512, LAYER>, grid, 512, 0, st, p, part);
+  }
+}
+
+template <typename T, bool LAYER>
+cudaError_t norm_backward_of(const NormLaunch& p, float* part, cudaStream_t st) {
+  constexpr int V = Elem<T>::kVec;
+  const bool vec = vectors_ok(p, true);
+  if (p.cols > kWideCols) {
+    if (p.dx) {
+      const dim3 grid((unsigned)std::min<uint64_t>(p.rows, (uint64_t)sm_count() * 2));
+      const cudaError_t e = vec ? launch_kernel(false, norm_backward_wide_kernel<T, V, LAYER>, grid, 1024, 0, st, p)
+                                : launch_kernel(false, norm_backward_wide_kernel<T, 1, LAYER>, grid, 1024, 0, st, p);
+      if (e != cudaSuccess) return e;
+    }
+    if (!part) return cudaSuccess;
+    const uint32_t n = backward_parts(p);
+    const dim3 grid((p.cols + 255u) / 256u, n);
+    return launch_kernel(p.dx != nullptr, norm_weight_sums_kernel<T, LAYER>, grid, 256, 0, st, p, part,
+                         (p.rows + n - 1) / n);
+  }
+  return vec ? norm_backward<T, V, 16 / V, LAYER>(p, part, st) : norm_backward<T, 1, 16, LAYER>(p, part, st);
+}
+
+template <typename T>
+cudaError_t column_sums(const float* part, uint32_t n_part, uint64_t stride, uint32_t cols, void* a, void* b,
+                        cudaStream_t st) {
+  const dim3 grid((cols + 31u) / 32u, b ? 2 : 1);
+  return launch_kernel(true, column_sums_kernel<T>, grid, 256, 0, st, part, n_part, stride, cols, static_cast<T*>(a),
+                       static_cast<T*>(b));
+}
+
+}  // namespace
+
+cudaError_t launch_norm(const NormLaunch& p, cudaStream_t st) {
+  if (p.dtype == MP_BF16)
+    return p.layer ? norm_forward_of<__nv_bfloat16, true>(p, st) : norm_forward_of<__nv_bfloat16, false>(p, st);
+  return p.layer ? norm_forward_of<float, true>(p, st) : norm_forward_of<float, false>(p, st);
+}
+
+size_t norm_backward_scratch(const NormLaunch& p) {
+  if (!p.dweight && !p.dbias) return 0;
+  return (size_t)backward_parts(p) * 2 * p.cols * sizeof(float);
+}
+
+cudaError_t launch_norm_backward(const NormLaunch& p, float* scratch, cudaStream_t st) {
+  cudaError_t e;
+  if (p.dtype == MP_BF16)
+    e = p.layer ? norm_backward_of<__nv_bfloat16, true>(p, scratch, st)
+                : norm_backward_of<__nv_bfloat16, false>(p, scratch, st);
+  else
+    e = p.layer ? norm_backward_of<float, true>(p, scratch, st) : norm_backward_of<float, false>(p, scratch, st);
+  if (e != cudaSuccess || !scratch) return e;
+  const uint32_t n = backward_parts(p);
+  return p.dtype == MP_BF16
+             ? column_sums<__nv_bfloat16>(scratch, n, 2ull * p.cols, p.cols, p.dweight, p.dbias, st)
+             : column_sums<float>(scratch, n, 2ull * p.cols, p.cols, p.dweight, p.dbias, st);
+}
+
+cudaError_t launch_column_sums(mp_dtype dtype, const float* part, uint32_t n_part, uint32_t cols, void* out,
+                               cudaStream_t st) {
+  return dtype == MP_BF16 ? column_sums<__nv_bfloat16>(part, n_part, cols, cols, out, nullptr, st)
+                          : column_sums<float>(part, n_part, cols, cols, out, nullptr, st);
+}
+
+}  // namespace mp
