@@ -465,51 +465,64 @@ def mp_plan_noalloc(K, n_blocks, n_groups, dtype, blk_len, blk_group, norm, maxa
 # ---- layer operators --------------------------------------------------------------------------------
 
 
-def _dtype_of(t) -> int:
+_torch = None        # the module, once a layer operator has been called
+_raw_stream = None   # device index -> the current stream's address
+_DTYPES = {}
+
+
+def _load_torch():
+    global _torch, _raw_stream
     import torch
-    if t.dtype == torch.bfloat16:
-        return MP_BF16
-    if t.dtype == torch.float32:
-        return MP_F32
-    raise ValueError(f"layer operators take bfloat16 or float32 tensors, not {t.dtype}")
+    _DTYPES.update({torch.bfloat16: MP_BF16, torch.float32: MP_F32})
+    # the current stream without an object around it: 0.1 instead of 3-6 us of a call that takes about 10
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _torch = torch
+    return torch
 
 
-def _matrix(name, t, shape, like):
+def _first(x, name="x"):
+    """torch, the dtype's number, the device and the shape of a call's first tensor"""
+    torch = _torch or _load_torch()
+    number = _DTYPES.get(x.dtype)
+    if number is None:
+        raise ValueError(f"layer operators take bfloat16 or float32 tensors, not {x.dtype}")
+    device = x.get_device()
+    if device < 0:
+        raise ValueError(f"{name} must be on a GPU")
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    return torch, number, device, shape
+
+
+def _matrix(name, t, shape, like, device):
     """(address, row stride) of a 2-d tensor of the given shape with contiguous rows; (None, 0) for None"""
     if t is None:
         return None, 0
-    if t.shape != shape or t.dtype != like.dtype:
-        raise ValueError(f"{name} must be {tuple(shape)} of {like.dtype}, not {tuple(t.shape)} of {t.dtype}")
-    _on_device(name, t, like)
-    rows, cols = shape
+    if t.shape != shape or t.dtype is not like:
+        raise ValueError(f"{name} must be {tuple(shape)} of {like}, not {tuple(t.shape)} of {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the GPU of the other tensors")
     row, step = t.stride()
+    rows, cols = shape
     if step != 1 and cols > 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
     return t.data_ptr(), row if rows > 1 else cols
 
 
-def _on_device(name, t, like):
-    if not t.is_cuda or t.device != like.device:
-        raise ValueError(f"{name} must be on the device of the other tensors, a GPU")
-
-
-def _vector(name, t, n, like, dtype=None):
+def _vector(name, t, n, dtype, device):
     if t is None:
         return None
-    if t.shape != (n,) or t.dtype != (dtype or like.dtype) or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be {n} contiguous elements of {dtype or like.dtype}")
-    _on_device(name, t, like)
+    if t.shape != (n,) or t.dtype is not dtype or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be {n} contiguous elements of {dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the GPU of the other tensors")
     return t.data_ptr()
 
 
-def _two_d(name, t):
-    if t.dim() != 2:
-        raise ValueError(f"{name} must have two dimensions")
-    return t.shape
-
-
-def _call(f, args, stream):
-    rc = f(ctypes.byref(args), _stream_ptr(stream))
+def _call(f, args, stream, device):
+    rc = f(ctypes.byref(args), _raw_stream(device) if stream is None else _stream_ptr(stream))
     if rc != MP_OK:
         _check(rc)
 
@@ -517,35 +530,36 @@ def _call(f, args, stream):
 def mp_norm(x, weight=None, bias=None, eps=1e-6, kind=MP_NORM_RMS, out=None, stream=None):
     """(y, mean, rstd): layer norm or RMS norm of the rows of x [rows, cols]; mean is None for MP_NORM_RMS.
     out: where y goes (may be x), else a new tensor"""
-    import torch
-    shape = _two_d("x", x)
+    torch, number, device, shape = _first(x)
     rows, cols = shape
-    layer = kind == MP_NORM_LAYER
-    y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
-    mean = torch.empty(rows, dtype=torch.float32, device=x.device) if layer else None
-    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    _call(lib().mp_norm,
-          _NormArgs(_dtype_of(x), kind, rows, cols, eps, *_matrix("x", x, shape, x), *_matrix("out", y, shape, x),
-                    _vector("weight", weight, cols, x), _vector("bias", bias, cols, x),
-                    mean.data_ptr() if layer else None, rstd.data_ptr()), stream)
+    dt, where = x.dtype, x.device
+    y = torch.empty(shape, dtype=dt, device=where) if out is None else out
+    mean = torch.empty(rows, dtype=torch.float32, device=where) if kind == MP_NORM_LAYER else None
+    rstd = torch.empty(rows, dtype=torch.float32, device=where)
+    _call((_lib or lib()).mp_norm,
+          _NormArgs(number, kind, rows, cols, eps, *_matrix("x", x, shape, dt, device), *_matrix("out", y, shape, dt, device),
+                    _vector("weight", weight, cols, dt, device), _vector("bias", bias, cols, dt, device),
+                    None if mean is None else mean.data_ptr(), rstd.data_ptr()), stream, device)
     return y, mean, rstd
 
 
 def mp_norm_backward(dy, x, weight, mean, rstd, kind=MP_NORM_RMS, bias=False, add=None, dx=None, stream=None):
     """(dx, dweight, dbias) of mp_norm; dweight is None without a weight, dbias unless `bias` is set.  add: a
     gradient that reaches x by another way, added to dx; dx: where it goes (may be add), else a new tensor"""
-    import torch
-    shape = _two_d("x", x)
+    torch, number, device, shape = _first(x)
     rows, cols = shape
+    dt, where = x.dtype, x.device
     if dx is None:
-        dx = torch.empty(shape, dtype=x.dtype, device=x.device)
-    dw = None if weight is None else torch.empty(cols, dtype=x.dtype, device=x.device)
-    db = torch.empty(cols, dtype=x.dtype, device=x.device) if bias else None
-    _call(lib().mp_norm_backward,
-          _NormBackwardArgs(_dtype_of(x), kind, rows, cols, *_matrix("dy", dy, shape, x), *_matrix("x", x, shape, x),
-                            *_matrix("add", add, shape, x), *_matrix("dx", dx, shape, x), _vector("weight", weight, cols, x),
-                            _vector("mean", mean, rows, x, torch.float32), _vector("rstd", rstd, rows, x, torch.float32),
-                            None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()), stream)
+        dx = torch.empty(shape, dtype=dt, device=where)
+    dw = None if weight is None else torch.empty(cols, dtype=dt, device=where)
+    db = torch.empty(cols, dtype=dt, device=where) if bias else None
+    _call((_lib or lib()).mp_norm_backward,
+          _NormBackwardArgs(number, kind, rows, cols, *_matrix("dy", dy, shape, dt, device),
+                            *_matrix("x", x, shape, dt, device), *_matrix("add", add, shape, dt, device),
+                            *_matrix("dx", dx, shape, dt, device), _vector("weight", weight, cols, dt, device),
+                            _vector("mean", mean, rows, torch.float32, device),
+                            _vector("rstd", rstd, rows, torch.float32, device),
+                            None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr()), stream, device)
     return dx, dw, db
 
 
@@ -553,16 +567,18 @@ def mp_linear(x, w, bias=None, act=MP_ACT_NONE, mul=None, residual=None, keep_pr
     """(y, pre): y = act(z) * mul + residual, z = x w^T + bias, for x [rows, in] and w [out, in]; pre is z where
     keep_pre is set (the backward pass needs it with an activation or a factor), else None.  out: where y goes
     (may be mul or residual), else a new tensor"""
-    import torch
-    rows, k = xs = _two_d("x", x)
-    n = _two_d("w", w)[0]
+    torch, number, device, xs = _first(x)
+    rows, k = xs
+    n = _first(w, "w")[3][0]
     shape = (rows, n)
-    y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
-    pre = torch.empty(shape, dtype=x.dtype, device=x.device) if keep_pre else None
-    _call(lib().mp_linear,
-          _LinearArgs(_dtype_of(x), act, rows, k, n, *_matrix("x", x, xs, x), *_matrix("w", w, (n, k), x),
-                      *_matrix("mul", mul, shape, x), *_matrix("residual", residual, shape, x), *_matrix("out", y, shape, x),
-                      *_matrix("pre", pre, shape, x), _vector("bias", bias, n, x)), stream)
+    dt, where = x.dtype, x.device
+    y = torch.empty(shape, dtype=dt, device=where) if out is None else out
+    pre = torch.empty(shape, dtype=dt, device=where) if keep_pre else None
+    _call((_lib or lib()).mp_linear,
+          _LinearArgs(number, act, rows, k, n, *_matrix("x", x, xs, dt, device), *_matrix("w", w, (n, k), dt, device),
+                      *_matrix("mul", mul, shape, dt, device), *_matrix("residual", residual, shape, dt, device),
+                      *_matrix("out", y, shape, dt, device), *_matrix("pre", pre, shape, dt, device),
+                      _vector("bias", bias, n, dt, device)), stream, device)
     return y, pre
 
 
@@ -570,42 +586,49 @@ def mp_linear_backward(dy, x, w, pre=None, act=MP_ACT_NONE, mul=None, bias=False
                        dw_add=None, dx=None, dw=None, stream=None):
     """(dx, dw, db, dmul) of mp_linear; db only where `bias` is set, dmul with a factor.  dx_add, dw_add: gradients
     to add to; dx, dw: where the results go (may be dx_add and dw_add), else new tensors"""
-    import torch
-    rows, k = xs = _two_d("x", x)
-    n = _two_d("w", w)[0]
+    torch, number, device, xs = _first(x)
+    rows, k = xs
+    n = _first(w, "w")[3][0]
     ws, shape = (n, k), (rows, n)
+    dt, where = x.dtype, x.device
     if not need_dx:
         dx = dx_add = None
     elif dx is None:
-        dx = torch.empty(xs, dtype=x.dtype, device=x.device)
+        dx = torch.empty(xs, dtype=dt, device=where)
     if not need_dw:
         dw = dw_add = None
     elif dw is None:
-        dw = torch.empty(ws, dtype=x.dtype, device=x.device)
-    db = torch.empty(n, dtype=x.dtype, device=x.device) if bias else None
-    dmul = None if mul is None else torch.empty(shape, dtype=x.dtype, device=x.device)
-    _call(lib().mp_linear_backward,
-          _LinearBackwardArgs(_dtype_of(x), act, rows, k, n, *_matrix("dy", dy, shape, x), *_matrix("x", x, xs, x),
-                              *_matrix("w", w, ws, x), *_matrix("pre", pre, shape, x), *_matrix("mul", mul, shape, x),
-                              *_matrix("dx_add", dx_add, xs, x), *_matrix("dw_add", dw_add, ws, x),
-                              *_matrix("dx", dx, xs, x), *_matrix("dw", dw, ws, x), *_matrix("dmul", dmul, shape, x),
-                              None if db is None else db.data_ptr()), stream)
+        dw = torch.empty(ws, dtype=dt, device=where)
+    db = torch.empty(n, dtype=dt, device=where) if bias else None
+    dmul = None if mul is None else torch.empty(shape, dtype=dt, device=where)
+    _call((_lib or lib()).mp_linear_backward,
+          _LinearBackwardArgs(number, act, rows, k, n, *_matrix("dy", dy, shape, dt, device),
+                              *_matrix("x", x, xs, dt, device), *_matrix("w", w, ws, dt, device),
+                              *_matrix("pre", pre, shape, dt, device), *_matrix("mul", mul, shape, dt, device),
+                              *_matrix("dx_add", dx_add, xs, dt, device), *_matrix("dw_add", dw_add, ws, dt, device),
+                              *_matrix("dx", dx, xs, dt, device), *_matrix("dw", dw, ws, dt, device),
+                              *_matrix("dmul", dmul, shape, dt, device), None if db is None else db.data_ptr()),
+          stream, device)
     return dx, dw, db, dmul
 
 
 def mp_coef_grad(fam: Family, index: Handle, plan: Handle, grad, out=None, stream=None):
     """[K, n_tensors] fp32: the gradient of the merge coefficients from the gradient of the merged weights (a flat tensor
     laid out like the base), over the blocks that the plan reads; its rows' sums are dL / dalpha.  AVG and TA"""
-    import torch
+    torch = _torch or _load_torch()
     shape = (fam.K, len(fam.tensors))
+    device = grad.get_device()
+    if device < 0:
+        raise ValueError("grad must be on a GPU")
     if out is None:
         out = torch.empty(shape, dtype=torch.float32, device=grad.device)
-    elif out.shape != shape or out.dtype != torch.float32 or not out.is_contiguous():
-        raise ValueError(f"out must be {shape} contiguous elements of float32")
+    elif out.shape != shape or out.dtype != torch.float32 or not out.is_contiguous() or out.get_device() != device:
+        raise ValueError(f"out must be {shape} contiguous elements of float32 on grad's GPU")
     span = fam.tensors[-1][0] + fam.tensors[-1][1]
-    if _dtype_of(grad) != fam.c.dtype or not grad.is_contiguous() or grad.numel() < span:
+    if _DTYPES.get(grad.dtype) != fam.c.dtype or not grad.is_contiguous() or grad.numel() < span:
         raise ValueError("grad must be a contiguous tensor of the family's type that spans its tensors")
-    _check(lib().mp_coef_grad(fam.ref(), index.ptr, plan.ptr, grad.data_ptr(), out.data_ptr(), _stream_ptr(stream)))
+    _check((_lib or lib()).mp_coef_grad(fam.ref(), index.ptr, plan.ptr, grad.data_ptr(), out.data_ptr(),
+                                        _raw_stream(device) if stream is None else _stream_ptr(stream)))
     return out
 
 

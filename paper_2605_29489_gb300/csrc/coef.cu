@@ -157,8 +157,8 @@ cudaError_t launch_coef(const CoefLaunch& p, float* part, cudaStream_t st) {
   if (items > 0x7FFFFFFFull) return cudaErrorInvalidValue;
   const dim3 grid((unsigned)items);
   cudaError_t e = p.dtype == MP_BF16
-                      ? launch_kernel(false, coef_kernel<__nv_bfloat16>, grid, kThreads, 0, st, p, part, per_block)
-                      : launch_kernel(false, coef_kernel<float>, grid, kThreads, 0, st, p, part, per_block);
+                      ? launch_kernel(true, coef_kernel<__nv_bfloat16>, grid, kThreads, 0, st, p, part, per_block)
+                      : launch_kernel(true, coef_kernel<float>, grid, kThreads, 0, st, p, part, per_block);
   if (e != cudaSuccess) return e;
   return launch_kernel(true, coef_sum_kernel, dim3(p.n_tensors, p.K), kThreads, 0, st, (const float*)part, items,
                        per_block, p.t_blk0, p.n_tensors, p.out);

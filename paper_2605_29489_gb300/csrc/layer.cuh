@@ -22,6 +22,7 @@ uint32_t stall_rounds();  // mp_debug_stall_pipeline
 struct Scratch {
   void* p = nullptr;
   cudaStream_t st = nullptr;
+  size_t planned = 0;
   Scratch() = default;
   Scratch(const Scratch&) = delete;
   Scratch& operator=(const Scratch&) = delete;
@@ -29,10 +30,22 @@ struct Scratch {
     st = s;
     return scratch_alloc(&p, bytes, s);
   }
+  // `bytes` more of what will be one allocation: their offset
+  size_t plan(size_t bytes) {
+    const size_t at = planned;
+    planned += (bytes + 255) / 256 * 256;
+    return at;
+  }
+  cudaError_t get(cudaStream_t s) { return planned ? get(planned, s) : cudaSuccess; }
+  void* at(size_t offset) const { return static_cast<char*>(p) + offset; }
   ~Scratch() {
     if (p) scratch_free(p, st);
   }
 };
+
+// Every kernel of the layer operators is launched so that it may take up its SMs while the kernel ahead of it on the
+// stream, whichever that is, still ends: each starts with kernel_begin (or kernel_wait and kernel_release), and
+// touches no memory before that.  A chain of single-token products saves about 2 us on each.
 
 // ---- element access ----------------------------------------------------------------------------
 template <typename T>
@@ -143,14 +156,18 @@ struct GemmLaunch {
   Epilogue e;
   uint32_t* err;
   uint32_t wait_limit, stall;
-  bool follows;
 };
 // whether an operand can be read as it is (bf16: 16-byte rows); else it goes through pack()
 bool gemm_operand_ok(mp_dtype dtype, const Mat& m);
 mp_status launch_gemm(const GemmLaunch& g, cudaStream_t st);
-// copies rows x cols elements into dst (row stride ldd)
-cudaError_t launch_repack(mp_dtype dtype, const Mat& m, uint64_t rows, uint64_t cols, void* dst, uint64_t ldd,
-                          cudaStream_t st);
+// up to two copies of rows x cols elements (zeros without a source) in one launch
+struct Copy {
+  Mat src;
+  uint64_t rows, cols;
+  void* dst;
+  uint64_t ldd;
+};
+cudaError_t launch_copies(mp_dtype dtype, const Copy* m, int n, cudaStream_t st);
 // the elementwise part of a linear layer's backward pass:
 // dz = dy * mul * act'(pre), dmul = dy * act(pre), db = column sums of dz
 struct DzLaunch {
@@ -166,10 +183,6 @@ struct DzLaunch {
 };
 size_t dz_scratch(const DzLaunch& p);
 cudaError_t launch_dz(const DzLaunch& p, float* scratch, cudaStream_t st);
-// dst[r, c] = src[r, c], or 0 without a source
-cudaError_t launch_copy_or_zero(mp_dtype dtype, const Mat& src, uint64_t rows, uint64_t cols, void* dst, uint64_t ldd,
-                                cudaStream_t st);
-
 // the sum over n_part rows of part [n_part][cols] into out: the second step of every column sum here
 cudaError_t launch_column_sums(mp_dtype dtype, const float* part, uint32_t n_part, uint32_t cols, void* out,
                                cudaStream_t st);

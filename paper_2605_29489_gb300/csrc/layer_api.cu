@@ -105,16 +105,34 @@ mp_status norm_shape(mp_dtype dtype, mp_norm_kind kind, uint64_t rows, uint64_t 
 
 cudaStream_t stream_of(mp_stream s) { return reinterpret_cast<cudaStream_t>(s); }
 
-// an operand that the tensor cores can read: itself, or a copy with rows of whole 16-byte vectors
-mp_status readable(mp_dtype dtype, Mat& m, uint64_t rows, uint64_t cols, Scratch& s, cudaStream_t cs) {
-  if (rows <= 1) m.ld = (cols + 7) / 8 * 8;  // no second row: any stride will do
-  if (gemm_operand_ok(dtype, m)) return MP_OK;
-  const uint64_t ld = (cols + 7) / 8 * 8;
-  cudaError_t e;
-  if ((e = s.get(rows * ld * 2, cs)) != cudaSuccess) return cuda_fail(e, "scratch");
-  if ((e = launch_repack(dtype, m, rows, cols, s.p, ld, cs)) != cudaSuccess) return cuda_fail(e, "copy kernel");
-  m = Mat{s.p, ld};
-  return MP_OK;
+// Operands that the tensor cores cannot read as they are (a bf16 matrix whose rows are not whole 16-byte vectors)
+// are copied to scratch, with rows that are.  need() takes note of one, copy() makes the copies and points the
+// operands at them.
+struct Repack {
+  Copy c[2];
+  Mat* m[2];
+  size_t at[2];
+  int n = 0;
+  void need(mp_dtype dtype, Mat& x, uint64_t rows, uint64_t cols, Scratch& s) {
+    if (rows <= 1) x.ld = (cols + 7) / 8 * 8;  // no second row: any stride will do
+    if (gemm_operand_ok(dtype, x)) return;
+    const uint64_t ld = (cols + 7) / 8 * 8;
+    c[n] = Copy{x, rows, cols, nullptr, ld};
+    m[n] = &x;
+    at[n++] = s.plan(rows * ld * 2);
+  }
+  cudaError_t copy(mp_dtype dtype, const Scratch& s, cudaStream_t cs) {
+    for (int k = 0; k < n; ++k) {
+      c[k].dst = s.at(at[k]);
+      *m[k] = Mat{c[k].dst, c[k].ldd};
+    }
+    return n ? launch_copies(dtype, c, n, cs) : cudaSuccess;
+  }
+};
+
+cudaError_t copy_or_zero(mp_dtype dtype, const Mat& src, uint64_t rows, uint64_t cols, void* dst, uint64_t ldd, cudaStream_t cs) {
+  const Copy c{src, rows, cols, dst, ldd};
+  return launch_copies(dtype, &c, 1, cs);
 }
 
 mp_status linear_shape(mp_dtype dtype, mp_act act, uint64_t rows, uint64_t in, uint64_t out) {
@@ -198,7 +216,7 @@ mp_status norm_backward(const mp_norm_backward_args& a, mp_stream stream) {
   TraceScope tr(MP_TRACE_NORM, cs);
   if (a.rows == 0) {  // sums over no rows
     for (void* d : {a.dweight, a.dbias})
-      if (d && (e = launch_copy_or_zero(a.dtype, Mat{}, 1, a.cols, d, a.cols, cs)) != cudaSuccess)
+      if (d && (e = copy_or_zero(a.dtype, Mat{}, 1, a.cols, d, a.cols, cs)) != cudaSuccess)
         return cuda_fail(e, "fill kernel");
     return MP_OK;
   }
@@ -249,13 +267,16 @@ mp_status linear(const mp_linear_args& a, mp_stream stream) {
   TraceScope tr(MP_TRACE_LINEAR, cs);
   GemmLaunch g = {};
   if ((st = error_word(g)) != MP_OK) return st;
-  Scratch sx, sw;
   g.dtype = a.dtype;
   g.a = Mat{a.x.data, a.x.ld};
   g.b = Mat{a.w.data, a.w.ld};
-  if ((st = readable(a.dtype, g.a, a.rows, a.in, sx, cs)) != MP_OK) return st;
-  if ((st = readable(a.dtype, g.b, a.out, a.in, sw, cs)) != MP_OK) return st;
-  g.follows = sx.p || sw.p;
+  Scratch s;
+  Repack re;
+  re.need(a.dtype, g.a, a.rows, a.in, s);
+  re.need(a.dtype, g.b, a.out, a.in, s);
+  cudaError_t e;
+  if ((e = s.get(cs)) != cudaSuccess) return cuda_fail(e, "scratch");
+  if ((e = re.copy(a.dtype, s, cs)) != cudaSuccess) return cuda_fail(e, "copy kernel");
   g.inner = a.in;
   g.e = Epilogue{a.rows, a.out, a.bias, a.act, Mat{a.mul.data, a.mul.ld}, Mat{a.residual.data, a.residual.ld},
                  a.y.data, a.pre.data, a.y.ld, a.pre.ld};
@@ -297,64 +318,63 @@ mp_status linear_backward(const mp_linear_backward_args& a, mp_stream stream) {
   cudaError_t e;
   if (a.rows == 0) {  // sums over no rows
     if (a.dw.data && !(a.dw_add.data == a.dw.data) &&
-        (e = launch_copy_or_zero(a.dtype, Mat{a.dw_add.data, a.dw_add.ld}, a.out, a.in, a.dw.data, a.dw.ld, cs)) != cudaSuccess)
+        (e = copy_or_zero(a.dtype, Mat{a.dw_add.data, a.dw_add.ld}, a.out, a.in, a.dw.data, a.dw.ld, cs)) != cudaSuccess)
       return cuda_fail(e, "fill kernel");
-    if (a.db && (e = launch_copy_or_zero(a.dtype, Mat{}, 1, a.out, a.db, a.out, cs)) != cudaSuccess)
+    if (a.db && (e = copy_or_zero(a.dtype, Mat{}, 1, a.out, a.db, a.out, cs)) != cudaSuccess)
       return cuda_fail(e, "fill kernel");
     return MP_OK;
   }
   GemmLaunch g = {};
   if ((st = error_word(g)) != MP_OK) return st;
   g.dtype = a.dtype;
-  Scratch sz, sp, sx, sw;
-  Mat dz{a.dy.data, a.dy.ld};
+  // the scratch: dz, its column sums, operands that have to be copied
   const bool products = a.dx.data || a.dw.data;
   const bool changed = a.act != MP_ACT_NONE || a.mul.data;
-  if (a.rows == 1) dz.ld = (a.out + 7) / 8 * 8;
+  Mat dz{a.dy.data, a.rows == 1 ? (a.out + 7) / 8 * 8 : a.dy.ld};
+  Mat w{a.w.data, a.w.ld}, x{a.x.data, a.x.ld};
   const bool own_dz = products && (changed || !gemm_operand_ok(a.dtype, dz));
-  if (own_dz || a.db || a.dmul.data) {
-    DzLaunch d = {};
-    d.dtype = a.dtype;
-    d.rows = a.rows;
-    d.cols = a.out;
-    d.dy = Mat{a.dy.data, a.dy.ld};
-    d.pre = Mat{a.pre.data, a.pre.ld};
-    d.mul = Mat{a.mul.data, a.mul.ld};
-    d.act = a.act;
-    d.dmul = a.dmul.data;
-    d.lddmul = a.dmul.ld;
-    d.db = a.db;
-    if (own_dz) {
-      d.lddz = (a.out + 7) / 8 * 8;
-      if ((e = sz.get(a.rows * d.lddz * es, cs)) != cudaSuccess) return cuda_fail(e, "scratch");
-      d.dz = sz.p;
-      dz = Mat{sz.p, d.lddz};
-    }
-    if (const size_t bytes = dz_scratch(d))
-      if ((e = sp.get(bytes, cs)) != cudaSuccess) return cuda_fail(e, "scratch");
-    if ((e = launch_dz(d, static_cast<float*>(sp.p), cs)) != cudaSuccess) return cuda_fail(e, "linear kernel");
-    g.follows = true;
+  DzLaunch d = {};
+  d.dtype = a.dtype;
+  d.rows = a.rows;
+  d.cols = a.out;
+  d.dy = Mat{a.dy.data, a.dy.ld};
+  d.pre = Mat{a.pre.data, a.pre.ld};
+  d.mul = Mat{a.mul.data, a.mul.ld};
+  d.act = a.act;
+  d.dmul = a.dmul.data;
+  d.lddmul = a.dmul.ld;
+  d.db = a.db;
+  Scratch s;
+  Repack re;
+  size_t dz_at = 0;
+  if (own_dz) {
+    d.lddz = (a.out + 7) / 8 * 8;
+    dz_at = s.plan(a.rows * d.lddz * es);
   }
+  const size_t part_at = s.plan(dz_scratch(d));
+  if (a.dx.data) re.need(a.dtype, w, a.out, a.in, s);
+  if (a.dw.data) re.need(a.dtype, x, a.rows, a.in, s);
+  if ((e = s.get(cs)) != cudaSuccess) return cuda_fail(e, "scratch");
+  if (own_dz) {
+    d.dz = s.at(dz_at);
+    dz = Mat{d.dz, d.lddz};
+  }
+  if ((own_dz || a.db || a.dmul.data) && (e = launch_dz(d, static_cast<float*>(s.at(part_at)), cs)) != cudaSuccess)
+    return cuda_fail(e, "linear kernel");
+  if ((e = re.copy(a.dtype, s, cs)) != cudaSuccess) return cuda_fail(e, "copy kernel");
+  g.a = dz;
   if (a.dx.data) {
-    g.a = dz;
-    g.b = Mat{a.w.data, a.w.ld};
-    if ((st = readable(a.dtype, g.b, a.out, a.in, sw, cs)) != MP_OK) return st;
-    g.a_t = false;
+    g.b = w;
     g.b_t = true;
     g.inner = a.out;
     g.e = Epilogue{a.rows, a.in, nullptr, MP_ACT_NONE, Mat{}, Mat{a.dx_add.data, a.dx_add.ld}, a.dx.data, nullptr, a.dx.ld, 0};
-    g.follows = g.follows || sw.p;
     if ((st = launch_gemm(g, cs)) != MP_OK) return st;
-    g.follows = true;
   }
   if (a.dw.data) {
-    g.a = dz;
-    g.b = Mat{a.x.data, a.x.ld};
-    if ((st = readable(a.dtype, g.b, a.rows, a.in, sx, cs)) != MP_OK) return st;
+    g.b = x;
     g.a_t = g.b_t = true;
     g.inner = a.rows;
     g.e = Epilogue{a.out, a.in, nullptr, MP_ACT_NONE, Mat{}, Mat{a.dw_add.data, a.dw_add.ld}, a.dw.data, nullptr, a.dw.ld, 0};
-    g.follows = g.follows || sx.p;
     if ((st = launch_gemm(g, cs)) != MP_OK) return st;
   }
   return MP_OK;

@@ -94,7 +94,7 @@ struct Epi {
   const T *bias, *mul, *res;
   uint64_t ldmul, ldres, ldy, ldpre;
   T *y, *pre;
-  uint32_t vec;
+  uint32_t vec, quad;  // quad: in whole vectors of four elements
 };
 
 template <typename T>
@@ -111,6 +111,34 @@ __device__ __forceinline__ void epi_one(const Epi<T>& e, uint32_t r, uint32_t c,
   if (e.mul) z *= Elem<T>::load(e.mul[r * e.ldmul + c]);
   if (e.res) z += Elem<T>::load(e.res[r * e.ldres + c]);
   e.y[r * e.ldy + c] = Elem<T>::store(z);
+}
+
+// four consecutive columns of a row, of which those below e.cols exist; quad: they are whole vectors of every matrix
+template <typename T>
+__device__ __forceinline__ void epi_quad(const Epi<T>& e, uint32_t r, uint32_t c, float* v, bool quad) {
+  constexpr bool FAST = sizeof(T) == 2;
+  if (!quad) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c + k < e.cols) epi_one(e, r, c + k, v[k]);
+    return;
+  }
+  Pack<T, 4> q, m, s;
+  if (e.mul) m = *reinterpret_cast<const Pack<T, 4>*>(e.mul + r * e.ldmul + c);
+  if (e.res) s = *reinterpret_cast<const Pack<T, 4>*>(e.res + r * e.ldres + c);
+  if (e.pre) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q.e[k] = Elem<T>::store(v[k]);
+    *reinterpret_cast<Pack<T, 4>*>(e.pre + r * e.ldpre + c) = q;
+  }
+  act_all<FAST, 4>(e.act, v);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (e.mul) v[k] *= Elem<T>::load(m.e[k]);
+    if (e.res) v[k] += Elem<T>::load(s.e[k]);
+    q.e[k] = Elem<T>::store(v[k]);
+  }
+  *reinterpret_cast<Pack<T, 4>*>(e.y + r * e.ldy + c) = q;
 }
 
 // N consecutive columns of a row, from c on (a multiple of N), of which those below e.cols exist
@@ -177,7 +205,8 @@ __device__ __forceinline__ void epi_run(const Epi<T>& e, uint32_t r, uint32_t c,
 
 constexpr int kBK = 64;                 // inner elements of a stage: one 128-byte swizzle span of bf16
 constexpr uint32_t kBoxT = 8192;        // bytes of an mn-major box: 64 k x 64 mn
-constexpr int kGemmThreads = 192;       // a TMA warp, a warp that issues products, four epilogue warps
+constexpr uint32_t kWarps = 6;
+constexpr int kGemmThreads = 32 * kWarps;       // a TMA warp, a warp that issues products, four epilogue warps
 
 using bf16 = __nv_bfloat16;
 
@@ -250,11 +279,12 @@ __global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_consta
     prefetch_map(&ma);
     prefetch_map(&mb);
   }
+  kernel_wait();  // what the kernel ahead wrote is read from here on
   if (warp == 1) tmem_alloc<1>(&tmem_at, kCols);
   umma_fence_before();
   __syncthreads();
   umma_fence_after();
-  kernel_begin();  // what the kernel ahead wrote is read from here on
+  kernel_release();
   const uint32_t tmem = tmem_at;
   if (warp == 0 && lane == 0) {
     uint32_t it = 0;
@@ -297,45 +327,59 @@ __global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_consta
   if (!ok && lane == 0) give_up(&abort, w);
   __syncthreads();  // all copies and products are over, or have been waited for
   umma_fence_after();
-  const uint32_t quad = warp & 3u, row = quad * 32u + lane;  // this thread's lane of tensor memory
-  const uint32_t c = (uint32_t)c0 + row;
+  // the CTA's sums to shared memory, [rows][128] (the stages are over), then every warp takes whole rows: a lane's
+  // four features from each CTA in turn, several rows' loads in flight
   const uint32_t n_r = min((uint32_t)BN, e.rows - (uint32_t)r0);
-  if (split == 1) {
-    if (warp >= 2 && !abort) {
-      const float bias = c < e.cols ? epi_bias(e, c) : 0.0f;
+  if (warp >= 2) {
+    const uint32_t quarter = warp & 3u, row = quarter * 32u + lane;  // this thread's lane of tensor memory
 #pragma unroll 1
-      for (uint32_t j0 = 0; j0 < n_r; j0 += 16) {
-        float v[16];
-        tmem_load16(tmem + ((quad * 32u) << 16) + j0, v);
-        if (c < e.cols) {
+    for (uint32_t j0 = 0; j0 < n_r; j0 += 16) {
+      float v[16];
+      tmem_load16(tmem + ((quarter * 32u) << 16) + j0, v);
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (j0 + j < n_r) epi_one(e, (uint32_t)r0 + j0 + j, c, v[j] + bias);
+      for (int j = 0; j < 16; ++j)
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + ((j0 + j) * 128u + row) * 4u), "f"(v[j]) : "memory");
+    }
+  }
+  if (split > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  const uint32_t c = (uint32_t)c0 + lane * 4u;
+  if (!abort && c < e.cols) {
+    float bias[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bias[k] = c + k < e.cols ? epi_bias(e, c + k) : 0.0f;
+    const bool whole = e.quad && c + 4 <= e.cols;
+    const uint32_t j1 = n_r * (rank + 1) / split;
+    constexpr int kAhead = 4;
+    for (uint32_t j = n_r * rank / split + warp; j < j1; j += kWarps * kAhead) {
+      float4 z[kAhead];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        z[a] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const uint32_t at = smem + (min(j + a * kWarps, j1 - 1) * 128u + lane * 4u) * 4u;
+        if (split == 1) {
+          z[a] = cluster_load4(at);
+        } else {
+          for (uint32_t q = 0; q < split; q += 2) {
+            const float4 u = cluster_load4(cluster_map(at, q)), v = cluster_load4(cluster_map(at, q + 1));
+            z[a].x = (z[a].x + u.x) + v.x;
+            z[a].y = (z[a].y + u.y) + v.y;
+            z[a].z = (z[a].z + u.z) + v.z;
+            z[a].w = (z[a].w + u.w) + v.w;
+          }
         }
       }
-    }
-  } else {
-    if (warp >= 2) {
-#pragma unroll 1
-      for (uint32_t j0 = 0; j0 < n_r; j0 += 16) {
-        float v[16];
-        tmem_load16(tmem + ((quad * 32u) << 16) + j0, v);
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + ((j0 + j) * 128u + row) * 4u), "f"(v[j]) : "memory");
-      }
+      for (int a = 0; a < kAhead; ++a)
+        if (j + a * kWarps < j1) {
+          float v[4] = {z[a].x + bias[0], z[a].y + bias[1], z[a].z + bias[2], z[a].w + bias[3]};
+          epi_quad(e, (uint32_t)r0 + j + a * kWarps, c, v, whole);
+        }
     }
-    cluster_sync();
-    if (warp >= 2 && !abort && c < e.cols) {
-      const float bias = epi_bias(e, c);
-      for (uint32_t j = n_r * rank / split; j < n_r * (rank + 1) / split; ++j) {
-        float z = 0.0f;
-        for (uint32_t q = 0; q < split; ++q) z += cluster_load(cluster_map(smem + (j * 128u + row) * 4u, q));
-        epi_one(e, (uint32_t)r0 + j, c, z + bias);
-      }
-    }
-    cluster_sync();  // nothing of this CTA is read any more
   }
+  if (split > 1) cluster_sync();  // nothing of this CTA is read any more
   umma_fence_before();
   __syncthreads();
   if (warp == 1) tmem_free<1>(tmem, kCols);
@@ -373,12 +417,13 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
     prefetch_map(&ma);
     prefetch_map(&mb);
   }
+  kernel_wait();
   if (warp == 1) tmem_alloc<CG>(&tmem_at, 512);
   umma_fence_before();
   __syncthreads();
   if (CG == 2) cluster_sync();  // the other CTA's barriers are there
   umma_fence_after();
-  kernel_begin();
+  kernel_release();
   const uint32_t tmem = tmem_at;
   const uint32_t n_tiles = tiles_r * tiles_c;
   auto place = [&](uint32_t t, int32_t& r0, int32_t& c0) {
@@ -486,69 +531,107 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
 
 // ---- fp32 products --------------------------------------------------------------------------------
 
-// out[r, c] = sum over k of a(r, k) b(c, k), element (r, k) at a + r * ar + k * ak: tiles of 64 x 64, 16 k at a time,
-// 4 x 4 sums a thread.  The next step's elements are on their way while this one's are multiplied.
-__global__ void __launch_bounds__(256) gemm_f32_kernel(const float* a, uint64_t ar, uint64_t ak, const float* b, uint64_t br,
-                                                       uint64_t bk, uint32_t inner, const Epi<float> e) {
+// out[r, c] = sum over k of a(r, k) b(c, k), element (r, k) at a + r * ar + k * ak: tiles of 64 R x 64 R, BK k at a time,
+// 4 R x 4 R sums a thread.  The next step's elements are on their way while this one's are multiplied.  With R = 1 the
+// inner dimension may be split over a cluster, whose sums are added over distributed shared memory in the CTAs'
+// order: a product of 512 x 512 x 512 is a chain of steps of about 1 us on 64 CTAs, a quarter of it on 256.
+template <int R, int BK>
+__global__ void __launch_bounds__(256, R == 1 ? 2 : 1) gemm_f32_kernel(const float* a, uint64_t ar, uint64_t ak, const float* b, uint64_t br,
+                                                       uint64_t bk, uint32_t inner, uint32_t k_each, const Epi<float> e) {
   kernel_begin();
-  __shared__ alignas(16) float sa[2][16][68], sb[2][16][68];
-  const uint32_t tiles_c = (e.cols + 63u) / 64u;
-  const uint32_t r0 = blockIdx.x / tiles_c * 64u, c0 = blockIdx.x % tiles_c * 64u;
+  constexpr uint32_t kTile = 64 * R, kPitch = kTile + 4;
+  constexpr int kLoads = kTile * BK / 256;
+  __shared__ alignas(16) float stage[2][2][BK][kPitch];  // [turn][operand]
+  const uint32_t rank = R == 1 ? cluster_rank() : 0u;
+  uint32_t split = 1;
+  if (R == 1) asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(split));
+  const uint32_t tiles_c = (e.cols + kTile - 1) / kTile, tile = blockIdx.x / split;
+  const uint32_t r0 = tile / tiles_c * kTile, c0 = tile % tiles_c * kTile;
+  const uint32_t first = rank * k_each, last = min(inner, first + k_each);
   const uint32_t t = threadIdx.x, tr = t / 16u, tc = t % 16u;
-  // element q of 4 of this thread's share of a tile: along k first where k is contiguous, else along the rows
+  // element q of this thread's share of a tile: along k first where k is contiguous, else along the rows
   auto spot = [&](uint64_t sk, int q, uint32_t& row, uint32_t& k) {
     if (sk == 1) {
-      k = t % 16u;
-      row = t / 16u + 16u * q;
+      k = t % BK;
+      row = t / BK + (256u / BK) * q;
     } else {
-      row = t % 64u;
-      k = t / 64u + 4u * q;
+      row = t % kTile;
+      k = t / kTile + (256u / kTile) * q;
     }
   };
-  float ra[4], rb[4];
+  float ra[kLoads], rb[kLoads];
   auto fetch = [&](uint32_t k0) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < kLoads; ++q) {
       uint32_t row, k;
       spot(ak, q, row, k);
-      ra[q] = r0 + row < e.rows && k0 + k < inner ? a[(r0 + row) * ar + (k0 + k) * ak] : 0.0f;
+      ra[q] = r0 + row < e.rows && k0 + k < last ? a[(r0 + row) * ar + (k0 + k) * ak] : 0.0f;
       spot(bk, q, row, k);
-      rb[q] = c0 + row < e.cols && k0 + k < inner ? b[(c0 + row) * br + (k0 + k) * bk] : 0.0f;
+      rb[q] = c0 + row < e.cols && k0 + k < last ? b[(c0 + row) * br + (k0 + k) * bk] : 0.0f;
     }
   };
   auto put = [&](int s) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < kLoads; ++q) {
       uint32_t row, k;
       spot(ak, q, row, k);
-      sa[s][k][row] = ra[q];
+      stage[s][0][k][row] = ra[q];
       spot(bk, q, row, k);
-      sb[s][k][row] = rb[q];
+      stage[s][1][k][row] = rb[q];
     }
   };
-  float acc[4][4] = {};
-  fetch(0);
+  float acc[4 * R][4 * R] = {};
+  fetch(first);
   put(0);
   __syncthreads();
   int s = 0;
-  for (uint32_t k0 = 0; k0 < inner; k0 += 16u, s ^= 1) {
-    const bool more = k0 + 16u < inner;
-    if (more) fetch(k0 + 16u);
+  for (uint32_t k0 = first; k0 < last; k0 += BK, s ^= 1) {
+    const bool more = k0 + BK < last;
+    if (more) fetch(k0 + BK);
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      float x[4], y[4];
-      *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(&sa[s][k][tr * 4u]);
-      *reinterpret_cast<float4*>(y) = *reinterpret_cast<const float4*>(&sb[s][k][tc * 4u]);
+    for (int k = 0; k < BK; ++k) {
+      float x[4 * R], y[4 * R];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int h = 0; h < R; ++h) {
+        *reinterpret_cast<float4*>(x + 4 * h) = *reinterpret_cast<const float4*>(&stage[s][0][k][h * 64 + tr * 4u]);
+        *reinterpret_cast<float4*>(y + 4 * h) = *reinterpret_cast<const float4*>(&stage[s][1][k][h * 64 + tc * 4u]);
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
+      for (int i = 0; i < 4 * R; ++i)
+#pragma unroll
+        for (int j = 0; j < 4 * R; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
     }
     if (more) put(s ^ 1);
     __syncthreads();
   }
+  if constexpr (R == 1) {
+    if (split > 1) {
+      float* sum = &stage[0][0][0][0];  // [64][64]
+      static_assert(sizeof(stage) >= 64 * 64 * 4, "the sums fit the stages");
 #pragma unroll
-  for (int i = 0; i < 4; ++i) epi_run<float, 4>(e, r0 + tr * 4u + i, c0 + tc * 4u, acc[i]);
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(sum + (tr * 4u + i) * 64u + tc * 4u) = *reinterpret_cast<float4*>(acc[i]);
+      cluster_sync();
+      for (uint32_t r = 64u * rank / split + tr; r < 64u * (rank + 1) / split; r += 16u) {
+        float v[4] = {};
+        const uint32_t at = su32(sum + r * 64u + tc * 4u);
+        for (uint32_t q = 0; q < split; ++q) {
+          const float4 u = cluster_load4(cluster_map(at, q));
+          v[0] += u.x;
+          v[1] += u.y;
+          v[2] += u.z;
+          v[3] += u.w;
+        }
+        epi_run<float, 4>(e, r0 + r, c0 + tc * 4u, v);
+      }
+      cluster_sync();
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4 * R; ++i)
+#pragma unroll
+    for (int h = 0; h < R; ++h)
+      epi_run<float, 4>(e, r0 + (i / 4) * 64u + tr * 4u + i % 4, c0 + h * 64u + tc * 4u, acc[i] + 4 * h);
 }
 
 // ---- elementwise and layout kernels ---------------------------------------------------------------
@@ -610,14 +693,29 @@ __global__ void __launch_bounds__(256) dz_kernel(const DzArgs<T> p) {
   }
 }
 
-// element (r, c) of src, or zeros, to dst; the columns from cols up to fill (rows of whole vectors) as zeros
+// copies (or zeros: no source) of up to two matrices, blockIdx.y saying which
 template <typename T>
-__global__ void __launch_bounds__(256) copy_kernel(const T* src, uint64_t lds, uint64_t rows, uint32_t cols, uint32_t fill,
-                                                   T* dst, uint64_t ldd) {
+struct CopyArgs {
+  const T* src;
+  T* dst;
+  uint64_t lds, ldd, rows;
+  uint32_t cols;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) copy_kernel(const CopyArgs<T> a, const CopyArgs<T> b) {
   kernel_begin();
-  for (uint64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (uint32_t c = threadIdx.x; c < fill; c += 256u)
-      dst[r * ldd + c] = src && c < cols ? src[r * lds + c] : T(0.0f);
+  const CopyArgs<T>& m = blockIdx.y ? b : a;
+  // a warp to a row, four elements of a lane in flight
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  for (uint64_t r = blockIdx.x * 8ull + warp; r < m.rows; r += gridDim.x * 8ull)
+    for (uint32_t c = lane; c < m.cols; c += 128u) {
+      T v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = m.src && c + 32u * k < m.cols ? m.src[r * m.lds + c + 32u * k] : T(0.0f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + 32u * k < m.cols) m.dst[r * m.ldd + c + 32u * k] = v[k];
+    }
 }
 
 // ---- launches -------------------------------------------------------------------------------------
@@ -658,7 +756,9 @@ mp_status make_map(CUtensorMap* map, const Mat& m, bool t, uint64_t n, uint64_t 
 template <typename T>
 Epi<T> epi_of(const Epilogue& e) {
   const size_t es = sizeof(T);
-  auto ok = [&](const void* p, uint64_t ld) { return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * es % 16 == 0); };
+  size_t unit = 16;
+  auto ok = [&](const void* p, uint64_t ld) { return !p || (reinterpret_cast<uintptr_t>(p) % unit == 0 && ld * es % unit == 0); };
+  auto all = [&] { return ok(e.bias, 0) && ok(e.mul.p, e.mul.ld) && ok(e.res.p, e.res.ld) && ok(e.y, e.ldy) && ok(e.pre, e.ldpre); };
   Epi<T> q;
   q.rows = (uint32_t)e.rows;
   q.cols = (uint32_t)e.cols;
@@ -672,7 +772,9 @@ Epi<T> epi_of(const Epilogue& e) {
   q.pre = static_cast<T*>(e.pre);
   q.ldy = e.ldy;
   q.ldpre = e.ldpre;
-  q.vec = ok(e.bias, 0) && ok(e.mul.p, e.mul.ld) && ok(e.res.p, e.res.ld) && ok(e.y, e.ldy) && ok(e.pre, e.ldpre);
+  q.vec = all();
+  unit = 4 * es;
+  q.quad = all();
   return q;
 }
 
@@ -686,13 +788,16 @@ int device_sms() {
 }
 
 template <typename... P, typename... A>
-cudaError_t launch_cluster(bool follows, void (*k)(P...), unsigned grid, unsigned cluster, size_t smem, cudaStream_t st,
+cudaError_t launch_cluster(void (*k)(P...), unsigned grid, unsigned threads, unsigned cluster, size_t smem, cudaStream_t st,
                            const A&... a) {
-  cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
+  if (smem > 0) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kGemmThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
@@ -703,39 +808,39 @@ cudaError_t launch_cluster(bool follows, void (*k)(P...), unsigned grid, unsigne
   at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
-  cfg.numAttrs = follows ? 2 : 1;
+  cfg.numAttrs = 2;
   count_launches(1);
   return cudaLaunchKernelEx(&cfg, k, P(a)...);
 }
 
 template <int BN, bool AT, bool BT>
 cudaError_t launch_split(const CUtensorMap& ma, const CUtensorMap& mb, const Epi<bf16>& e, uint32_t kb, unsigned split,
-                         int stages, bool follows, const Wait& w, cudaStream_t st) {
+                         int stages, const Wait& w, cudaStream_t st) {
   const uint32_t tiles_r = (e.rows + BN - 1) / BN, tiles_c = (e.cols + 127u) / 128u;
   const size_t smem = (size_t)stages * (128 * 128 + BN * 128) + 1024;
-  return launch_cluster(follows, split_kernel<BN, AT, BT>, tiles_r * tiles_c * split, split, smem, st, ma, mb, e, kb, tiles_r,
+  return launch_cluster(split_kernel<BN, AT, BT>, tiles_r * tiles_c * split, kGemmThreads, split, smem, st, ma, mb, e, kb, tiles_r,
                         stages, w);
 }
 
 template <bool AT, bool BT>
 cudaError_t launch_split_of(int bn, const CUtensorMap& ma, const CUtensorMap& mb, const Epi<bf16>& e, uint32_t kb,
-                            unsigned split, int stages, bool follows, const Wait& w, cudaStream_t st) {
+                            unsigned split, int stages, const Wait& w, cudaStream_t st) {
   if constexpr (!BT) {
-    if (bn == 16) return launch_split<16, AT, BT>(ma, mb, e, kb, split, stages, follows, w, st);
-    if (bn == 32) return launch_split<32, AT, BT>(ma, mb, e, kb, split, stages, follows, w, st);
-    if (bn == 64) return launch_split<64, AT, BT>(ma, mb, e, kb, split, stages, follows, w, st);
+    if (bn == 16) return launch_split<16, AT, BT>(ma, mb, e, kb, split, stages, w, st);
+    if (bn == 32) return launch_split<32, AT, BT>(ma, mb, e, kb, split, stages, w, st);
+    if (bn == 64) return launch_split<64, AT, BT>(ma, mb, e, kb, split, stages, w, st);
   }
-  return launch_split<128, AT, BT>(ma, mb, e, kb, split, stages, follows, w, st);
+  return launch_split<128, AT, BT>(ma, mb, e, kb, split, stages, w, st);
 }
 
 template <int CG, bool AT, bool BT>
-cudaError_t launch_big(const CUtensorMap& ma, const CUtensorMap& mb, const Epi<bf16>& e, uint32_t kb, bool follows,
+cudaError_t launch_big(const CUtensorMap& ma, const CUtensorMap& mb, const Epi<bf16>& e, uint32_t kb,
                        const Wait& w, cudaStream_t st) {
   const uint32_t tiles_r = (e.rows + 128u * CG - 1) / (128u * CG), tiles_c = (e.cols + 255u) / 256u;
   const uint64_t tiles = (uint64_t)tiles_r * tiles_c;
   const unsigned groups = (unsigned)std::min<uint64_t>(tiles, (uint64_t)device_sms() / CG);
   const size_t smem = CG == 2 ? 6 * 32768 + 1024 : 4 * 49152 + 1024;
-  return launch_cluster(follows, gemm_kernel<CG, AT, BT>, groups * CG, CG, smem, st, ma, mb, e, kb, tiles_r, tiles_c, w);
+  return launch_cluster(gemm_kernel<CG, AT, BT>, groups * CG, kGemmThreads, CG, smem, st, ma, mb, e, kb, tiles_r, tiles_c, w);
 }
 
 mp_status gemm_bf16(const GemmLaunch& g, cudaStream_t st) {
@@ -755,25 +860,46 @@ mp_status gemm_bf16(const GemmLaunch& g, cudaStream_t st) {
   const Wait w = {g.err, g.wait_limit ? g.wait_limit : kWaitLimit, g.stall};
   cudaError_t r;
   if (big) {
-    r = g.a_t ? launch_big<2, true, true>(ma, mb, e, kb, g.follows, w, st)
-        : g.b_t ? launch_big<2, false, true>(ma, mb, e, kb, g.follows, w, st)
-                : launch_big<2, false, false>(ma, mb, e, kb, g.follows, w, st);
+    r = g.a_t ? launch_big<2, true, true>(ma, mb, e, kb, w, st)
+        : g.b_t ? launch_big<2, false, true>(ma, mb, e, kb, w, st)
+                : launch_big<2, false, false>(ma, mb, e, kb, w, st);
   } else {
     const uint64_t tiles = ((g.e.rows + bn - 1) / bn) * ((g.e.cols + 127) / 128);
     unsigned split = 1;
     while (split < 8 && tiles * split * 2 <= sms * 2 && kb >= 4 * split) split *= 2;
     const int stage = 128 * 128 + bn * 128;
     const int stages = std::min(6, 100 * 1024 / stage);
-    r = g.a_t ? launch_split_of<true, true>(bn, mb, ma, e, kb, split, stages, g.follows, w, st)
-        : g.b_t ? launch_split_of<true, false>(bn, mb, ma, e, kb, split, stages, g.follows, w, st)
-                : launch_split_of<false, false>(bn, mb, ma, e, kb, split, stages, g.follows, w, st);
+    r = g.a_t ? launch_split_of<true, true>(bn, mb, ma, e, kb, split, stages, w, st)
+        : g.b_t ? launch_split_of<true, false>(bn, mb, ma, e, kb, split, stages, w, st)
+                : launch_split_of<false, false>(bn, mb, ma, e, kb, split, stages, w, st);
   }
+  return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
+}
+
+mp_status gemm_f32(const GemmLaunch& g, cudaStream_t st) {
+  const Epi<float> e = epi_of<float>(g.e);
+  auto tiles_of = [&](uint64_t n) { return ((g.e.rows + n - 1) / n) * ((g.e.cols + n - 1) / n); };
+  const uint64_t sms = (uint64_t)device_sms(), one = 1;
+  const bool large = tiles_of(128) >= sms;  // tiles of 128 fill the GPU
+  const uint64_t tiles = tiles_of(large ? 128 : 64);
+  if (tiles > 0x7FFFFFFFull) {
+    set_static_error("the output has too many tiles");
+    return MP_ERR_UNSUPPORTED;
+  }
+  unsigned split = 1;
+  while (!large && split < 8 && tiles * split * 2 <= sms * 2 && g.inner >= 128ull * split) split *= 2;
+  const uint32_t inner = (uint32_t)g.inner, each = (uint32_t)(((g.inner + split - 1) / split + 31) / 32 * 32);
+  const float *a = static_cast<const float*>(g.a.p), *b = static_cast<const float*>(g.b.p);
+  const uint64_t ar = g.a_t ? one : g.a.ld, ak = g.a_t ? g.a.ld : one, br = g.b_t ? one : g.b.ld, bk = g.b_t ? g.b.ld : one;
+  const cudaError_t r =
+      large ? launch_kernel(true, gemm_f32_kernel<2, 16>, dim3((unsigned)tiles), 256, 0, st, a, ar, ak, b, br, bk, inner, inner, e)
+            : launch_cluster(gemm_f32_kernel<1, 32>, (unsigned)tiles * split, 256, split, 0, st, a, ar, ak, b, br, bk, inner, each, e);
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
 
 template <typename T, int V, int ACT>
 cudaError_t dz_launch(const DzArgs<T>& a, dim3 grid, cudaStream_t st) {
-  return launch_kernel(false, dz_kernel<T, V, ACT>, grid, 256, 0, st, a);
+  return launch_kernel(true, dz_kernel<T, V, ACT>, grid, 256, 0, st, a);
 }
 
 constexpr uint32_t kDzParts = 64;  // runs of rows at most: their column sums are read again
@@ -830,17 +956,7 @@ bool gemm_operand_ok(mp_dtype dtype, const Mat& m) {
 
 mp_status launch_gemm(const GemmLaunch& g, cudaStream_t st) {
   if (g.dtype == MP_BF16) return gemm_bf16(g, st);
-  const Epi<float> e = epi_of<float>(g.e);
-  const uint64_t tiles = ((g.e.rows + 63) / 64) * ((g.e.cols + 63) / 64);
-  if (tiles > 0x7FFFFFFFull) {
-    set_static_error("the output has too many tiles");
-    return MP_ERR_UNSUPPORTED;
-  }
-  const uint64_t one = 1;
-  const cudaError_t r = launch_kernel(
-      g.follows, gemm_f32_kernel, dim3((unsigned)tiles), 256, 0, st, static_cast<const float*>(g.a.p), g.a_t ? one : g.a.ld,
-      g.a_t ? g.a.ld : one, static_cast<const float*>(g.b.p), g.b_t ? one : g.b.ld, g.b_t ? g.b.ld : one, (uint32_t)g.inner, e);
-  return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
+  return gemm_f32(g, st);
 }
 
 size_t dz_scratch(const DzLaunch& p) {
@@ -853,18 +969,21 @@ cudaError_t launch_dz(const DzLaunch& p, float* scratch, cudaStream_t st) {
   return vec ? dz_of<float, 4>(p, scratch, st) : dz_of<float, 1>(p, scratch, st);
 }
 
-cudaError_t launch_repack(mp_dtype dtype, const Mat& m, uint64_t rows, uint64_t cols, void* dst, uint64_t ldd, cudaStream_t st) {
-  const dim3 grid((unsigned)std::min<uint64_t>(rows, 8ull * device_sms()));
-  const uint32_t c = (uint32_t)cols;
-  return dtype == MP_BF16 ? launch_kernel(false, copy_kernel<bf16>, grid, 256, 0, st, static_cast<const bf16*>(m.p), m.ld, rows,
-                                          c, c, static_cast<bf16*>(dst), ldd)
-                          : launch_kernel(false, copy_kernel<float>, grid, 256, 0, st, static_cast<const float*>(m.p), m.ld,
-                                          rows, c, c, static_cast<float*>(dst), ldd);
+template <typename T>
+cudaError_t copy_of(const Copy* m, int n, cudaStream_t st) {
+  CopyArgs<T> a[2] = {};
+  uint64_t rows = 0;
+  for (int k = 0; k < n; ++k) {
+    a[k] = CopyArgs<T>{static_cast<const T*>(m[k].src.p), static_cast<T*>(m[k].dst), m[k].src.ld, m[k].ldd, m[k].rows,
+                       (uint32_t)m[k].cols};
+    rows = std::max(rows, m[k].rows);
+  }
+  const dim3 grid((unsigned)std::min<uint64_t>((rows + 7) / 8, 8ull * device_sms()), n);
+  return launch_kernel(true, copy_kernel<T>, grid, 256, 0, st, a[0], a[1]);
 }
 
-cudaError_t launch_copy_or_zero(mp_dtype dtype, const Mat& src, uint64_t rows, uint64_t cols, void* dst, uint64_t ldd,
-                                cudaStream_t st) {
-  return launch_repack(dtype, src, rows, cols, dst, ldd, st);
+cudaError_t launch_copies(mp_dtype dtype, const Copy* m, int n, cudaStream_t st) {
+  return dtype == MP_BF16 ? copy_of<bf16>(m, n, st) : copy_of<float>(m, n, st);
 }
 
 }  // namespace mp

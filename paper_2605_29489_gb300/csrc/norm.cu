@@ -29,24 +29,25 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// sums of two values over the ROWT threads of a row; red: 2 floats per warp of the CTA.  Every thread gets the same
-// bits: with more than one warp each adds the warps' sums in the same order.
-template <int ROWT>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2* red) {
+// sums of two values over the ROWT threads of a row; red: two sets of a pair per warp of the CTA, taken in turn (turn
+// counts the calls), so that one barrier is enough.  Every thread gets the same bits: with more than one warp each adds
+// the warps' sums in the same order.
+template <int ROWT, int WARPS>
+__device__ __forceinline__ float2 row_sum2(float a, float b, float2 (*red)[WARPS], uint32_t& turn) {
   a = warp_sum(a);
   b = warp_sum(b);
   if constexpr (ROWT > 32) {
     constexpr int W = ROWT / 32;
     const int warp = threadIdx.x >> 5, first = (threadIdx.x / ROWT) * W;
-    if ((threadIdx.x & 31) == 0) red[warp] = make_float2(a, b);
+    float2* set = red[turn++ & 1u];
+    if ((threadIdx.x & 31) == 0) set[warp] = make_float2(a, b);
     __syncthreads();
     a = b = 0.0f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      a += red[first + w].x;
-      b += red[first + w].y;
+      a += set[first + w].x;
+      b += set[first + w].y;
     }
-    __syncthreads();
   }
   return make_float2(a, b);
 }
@@ -57,36 +58,48 @@ constexpr int cta_of() {
   return ROWT < 128 ? 128 : ROWT;
 }
 
+// The next row's loads are on their way while this one's sums are taken: the time is that of the bytes, not of the
+// steps from the first load of a row to its last store.
 template <typename T, int V, int NV, int ROWT, bool LAYER>
 __global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_kernel(const NormLaunch p) {
   kernel_begin();
   constexpr int kRows = cta_of<ROWT>() / ROWT;
-  __shared__ float2 red[cta_of<ROWT>() / 32];
+  __shared__ float2 red[2][cta_of<ROWT>() / 32];
+  uint32_t turn = 0;
   const int lane = threadIdx.x % ROWT;
   const T* w = static_cast<const T*>(p.weight);
   const T* b = static_cast<const T*>(p.bias);
   const float inv = 1.0f / (float)p.cols;
+  const uint64_t step = (uint64_t)gridDim.x * kRows;
+  Pack<T, V> q[NV];
+  auto fetch = [&](uint64_t r) {
+    const T* x = static_cast<const T*>(p.x) + r * p.ldx;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+      if (c < p.cols) q[k] = load_pack<T, V>(x + c);
+    }
+  };
+  uint64_t r0 = (uint64_t)blockIdx.x * kRows;
+  if (r0 + threadIdx.x / ROWT < p.rows) fetch(r0 + threadIdx.x / ROWT);
   // the rows of a CTA go on together (its threads meet at the sums): r0 is the same for all of them
-  for (uint64_t r0 = (uint64_t)blockIdx.x * kRows; r0 < p.rows; r0 += (uint64_t)gridDim.x * kRows) {
+  for (; r0 < p.rows; r0 += step) {
     const uint64_t r = r0 + threadIdx.x / ROWT;
-    const bool live = r < p.rows;
-    const T* x = static_cast<const T*>(p.x) + (live ? r : r0) * p.ldx;
     float v[NV * V];
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
-      Pack<T, V> q;
-      if (c < p.cols) q = load_pack<T, V>(x + c);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        v[k * V + e] = c < p.cols ? Elem<T>::load(q.e[e]) : 0.0f;
+        v[k * V + e] = c < p.cols ? Elem<T>::load(q[k].e[e]) : 0.0f;
         s = LAYER ? s + v[k * V + e] : fmaf(v[k * V + e], v[k * V + e], s);
       }
     }
+    if (r + step < p.rows) fetch(r + step);
     float mu = 0.0f;
     if (LAYER) {
-      mu = row_sum2<ROWT>(s, 0.0f, red).x * inv;
+      mu = row_sum2<ROWT>(s, 0.0f, red, turn).x * inv;
       s = 0.0f;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
@@ -98,9 +111,9 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_kernel(const NormLaunc
         }
       }
     }
-    const float var = row_sum2<ROWT>(s, 0.0f, red).x * inv;
+    const float var = row_sum2<ROWT>(s, 0.0f, red, turn).x * inv;
     const float rstd = 1.0f / sqrtf(var + p.eps);
-    if (live) {
+    if (r < p.rows) {
       if (lane == 0) {
         if (p.rstd) p.rstd[r] = rstd;
         if (LAYER && p.mean) p.mean[r] = mu;
@@ -131,7 +144,8 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_kernel(const NormLaunc
 template <typename T, int V, bool LAYER>
 __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) {
   kernel_begin();
-  __shared__ float2 red[32];
+  __shared__ float2 red[2][32];
+  uint32_t turn = 0;
   const T* w = static_cast<const T*>(p.weight);
   const T* b = static_cast<const T*>(p.bias);
   const float inv = 1.0f / (float)p.cols;
@@ -144,7 +158,7 @@ __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) 
 #pragma unroll
         for (int e = 0; e < V; ++e) s += Elem<T>::load(q.e[e]);
       }
-      mu = row_sum2<1024>(s, 0.0f, red).x * inv;
+      mu = row_sum2<1024>(s, 0.0f, red, turn).x * inv;
       s = 0.0f;
     }
     for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
@@ -155,7 +169,7 @@ __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) 
         s = fmaf(t, t, s);
       }
     }
-    const float rstd = 1.0f / sqrtf(row_sum2<1024>(s, 0.0f, red).x * inv + p.eps);
+    const float rstd = 1.0f / sqrtf(row_sum2<1024>(s, 0.0f, red, turn).x * inv + p.eps);
     if (threadIdx.x == 0) {
       if (p.rstd) p.rstd[r] = rstd;
       if (LAYER && p.mean) p.mean[r] = mu;
@@ -179,47 +193,66 @@ __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) 
 }
 
 // dx of the rows of a CTA and its sums for dw (part [2 * cta]) and db (part [2 * cta + 1]); sums: whether those
-// are wanted.  NV * V is 16 at most: x and dy stay as they are stored, the sums take two registers a column.
+// are wanted.  A thread has 8 columns (NV * V): x, dy and the next row's stay as they are stored, the sums take two
+// registers a column, and 1024 threads fit an SM.
 template <typename T, int V, int NV, int ROWT, bool LAYER>
-__global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_backward_kernel(const NormLaunch p, float* part) {
+__global__ void __launch_bounds__(cta_of<ROWT>(), 1024 / cta_of<ROWT>()) norm_backward_kernel(const NormLaunch p, float* part) {
   kernel_begin();
   constexpr int kRows = cta_of<ROWT>() / ROWT;
-  __shared__ float2 red[cta_of<ROWT>() / 32];
+  __shared__ float2 red[2][cta_of<ROWT>() / 32];
+  uint32_t turn = 0;
   const int lane = threadIdx.x % ROWT;
   const T* w = static_cast<const T*>(p.weight);
   const float inv = 1.0f / (float)p.cols;
+  const uint64_t step = (uint64_t)gridDim.x * kRows;
   float aw[NV * V] = {}, ab[NV * V] = {};
-  for (uint64_t r0 = (uint64_t)blockIdx.x * kRows; r0 < p.rows; r0 += (uint64_t)gridDim.x * kRows) {
-    const uint64_t r = r0 + threadIdx.x / ROWT;
-    const bool live = r < p.rows;
-    const uint64_t rr = live ? r : r0;
-    const T* x = static_cast<const T*>(p.x) + rr * p.ldx;
-    const T* dy = static_cast<const T*>(p.dy) + rr * p.lddy;
-    const float mu = LAYER ? p.mean[rr] : 0.0f, rstd = p.rstd[rr];
-    Pack<T, V> xq[NV], dq[NV];
+  Pack<T, V> xn[NV], dn[NV];  // the next row
+  float mun = 0.0f, rstdn = 0.0f;
+  auto fetch = [&](uint64_t r) {
+    const T* x = static_cast<const T*>(p.x) + r * p.ldx;
+    const T* dy = static_cast<const T*>(p.dy) + r * p.lddy;
+    mun = LAYER ? p.mean[r] : 0.0f;
+    rstdn = p.rstd[r];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
       if (c < p.cols) {
-        xq[k] = load_pack<T, V>(x + c);
-        dq[k] = load_pack<T, V>(dy + c);
+        xn[k] = load_pack<T, V>(x + c);
+        dn[k] = load_pack<T, V>(dy + c);
       }
     }
-    float s1 = 0.0f, s2 = 0.0f;
+  };
+  uint64_t r0 = (uint64_t)blockIdx.x * kRows;
+  if (r0 + threadIdx.x / ROWT < p.rows) fetch(r0 + threadIdx.x / ROWT);
+  for (; r0 < p.rows; r0 += step) {
+    const uint64_t r = r0 + threadIdx.x / ROWT;
+    const bool live = r < p.rows;
+    const float mu = mun, rstd = rstdn;
+    Pack<T, V> xq[NV], dq[NV], aq[NV];
+    const T* add = p.add && live ? static_cast<const T*>(p.add) + r * p.ldadd : nullptr;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
-      if (c < p.cols) {
-        Pack<T, V> wq;
-        if (w) wq = load_pack<T, V>(w + c);
+      xq[k] = xn[k];
+      dq[k] = dn[k];
+      if (add && c < p.cols) aq[k] = load_pack<T, V>(add + c);
+    }
+    if (r + step < p.rows) fetch(r + step);
+    float s1 = 0.0f, s2 = 0.0f;
+    if (live) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float d = Elem<T>::load(dq[k].e[e]);
-          const float h = (Elem<T>::load(xq[k].e[e]) - mu) * rstd;
-          const float g = w ? d * Elem<T>::load(wq.e[e]) : d;
-          s1 = fmaf(g, h, s1);
-          if (LAYER) s2 += g;
-          if (live) {
+      for (int k = 0; k < NV; ++k) {
+        const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+        if (c < p.cols) {
+          Pack<T, V> wq;
+          if (w) wq = load_pack<T, V>(w + c);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float d = Elem<T>::load(dq[k].e[e]);
+            const float h = (Elem<T>::load(xq[k].e[e]) - mu) * rstd;
+            const float g = w ? d * Elem<T>::load(wq.e[e]) : d;
+            s1 = fmaf(g, h, s1);
+            if (LAYER) s2 += g;
             aw[k * V + e] = fmaf(d, h, aw[k * V + e]);
             if (LAYER) ab[k * V + e] += d;
           }
@@ -227,18 +260,16 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_backward_kernel(const 
       }
     }
     if (!p.dx) continue;
-    const float2 m = row_sum2<ROWT>(s1, s2, red);
+    const float2 m = row_sum2<ROWT>(s1, s2, red, turn);
     const float m1 = m.x * inv, m2 = m.y * inv;
     if (live) {
       T* dx = static_cast<T*>(p.dx) + r * p.lddx;
-      const T* add = p.add ? static_cast<const T*>(p.add) + r * p.ldadd : nullptr;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
         if (c < p.cols) {
-          Pack<T, V> o, wq, aq;
+          Pack<T, V> o, wq;
           if (w) wq = load_pack<T, V>(w + c);
-          if (add) aq = load_pack<T, V>(add + c);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             const float d = Elem<T>::load(dq[k].e[e]);
@@ -246,7 +277,7 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_backward_kernel(const 
             float t = w ? d * Elem<T>::load(wq.e[e]) : d;
             if (LAYER) t -= m2;
             t = (t - h * m1) * rstd;
-            if (add) t += Elem<T>::load(aq.e[e]);
+            if (add) t += Elem<T>::load(aq[k].e[e]);
             o.e[e] = Elem<T>::store(t);
           }
           store_pack<T, V>(dx + c, o);
@@ -295,7 +326,8 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_backward_kernel(const 
 template <typename T, int V, bool LAYER>
 __global__ void __launch_bounds__(1024, 1) norm_backward_wide_kernel(const NormLaunch p) {
   kernel_begin();
-  __shared__ float2 red[32];
+  __shared__ float2 red[2][32];
+  uint32_t turn = 0;
   const T* w = static_cast<const T*>(p.weight);
   const float inv = 1.0f / (float)p.cols;
   for (uint64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
@@ -316,7 +348,7 @@ __global__ void __launch_bounds__(1024, 1) norm_backward_wide_kernel(const NormL
         s2 += g;
       }
     }
-    const float2 m = row_sum2<1024>(s1, s2, red);
+    const float2 m = row_sum2<1024>(s1, s2, red, turn);
     const float m1 = m.x * inv, m2 = LAYER ? m.y * inv : 0.0f;
     T* dx = static_cast<T*>(p.dx) + r * p.lddx;
     for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
@@ -356,35 +388,33 @@ __global__ void __launch_bounds__(256) norm_weight_sums_kernel(const NormLaunch 
   part[((uint64_t)blockIdx.y * 2 + 1) * p.cols + c] = ab;
 }
 
-// out[c] = sum over q of part[q * stride + c], 32 columns to a CTA: eight warps take every eighth part each, then
+// out[c] = sum over q of part[q * stride + c], 32 columns to a CTA: its 32 warps take every 32nd part each, then
 // their sums are added in order
 template <typename T>
-__global__ void __launch_bounds__(256) column_sums_kernel(const float* part, uint32_t n_part, uint64_t stride,
-                                                          uint32_t cols, T* out, T* out2) {
+__global__ void __launch_bounds__(1024) column_sums_kernel(const float* part, uint32_t n_part, uint64_t stride,
+                                                           uint32_t cols, T* out, T* out2) {
   kernel_begin();
-  __shared__ float s[8][33];
-  const uint32_t c = blockIdx.x * 32u + (threadIdx.x & 31u), w = threadIdx.x >> 5;
+  __shared__ float s[32][33];
+  const uint32_t lane = threadIdx.x & 31u, w = threadIdx.x >> 5, c = blockIdx.x * 32u + lane;
   const float* src = part + (blockIdx.y ? cols : 0u);
   T* dst = blockIdx.y ? out2 : out;
-  float a0 = 0.0f, a1 = 0.0f, a2 = 0.0f, a3 = 0.0f;
-  if (c < cols && dst) {
+  if (!dst) return;
+  float a[4] = {};
+  if (c < cols) {
     uint32_t q = w;
-    for (; q + 24u < n_part; q += 32u) {
-      a0 += src[q * stride + c];
-      a1 += src[(q + 8u) * stride + c];
-      a2 += src[(q + 16u) * stride + c];
-      a3 += src[(q + 24u) * stride + c];
-    }
-    for (; q < n_part; q += 8u) a0 += src[q * stride + c];
-  }
-  s[w][threadIdx.x & 31u] = (a0 + a1) + (a2 + a3);
-  __syncthreads();
-  if (w == 0 && c < cols && dst) {
-    float t = 0.0f;
+    for (; q + 96u < n_part; q += 128u) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) t += s[k][threadIdx.x];
-    dst[c] = Elem<T>::store(t);
+      for (int k = 0; k < 4; ++k) a[k] += src[(q + 32u * k) * stride + c];
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (q + 32u * k < n_part) a[k] += src[(q + 32u * k) * stride + c];
   }
+  s[w][lane] = (a[0] + a[1]) + (a[2] + a[3]);
+  __syncthreads();
+  // warp w adds up column w
+  const float t = warp_sum(s[lane][w]);
+  if (lane == 0 && blockIdx.x * 32u + w < cols) dst[blockIdx.x * 32u + w] = Elem<T>::store(t);
 }
 
 bool aligned16(const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15u) == 0; }
@@ -421,11 +451,11 @@ cudaError_t norm_forward(const NormLaunch& p, cudaStream_t st) {
   const uint64_t most = (uint64_t)sm_count() * (2048 / std::max(t, 128));
   const dim3 grid((unsigned)std::min(ctas, most));
   switch (t) {
-    case 32: return launch_kernel(false, norm_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p);
-    case 128: return launch_kernel(false, norm_kernel<T, V, NV, 128, LAYER>, grid, 128, 0, st, p);
-    case 256: return launch_kernel(false, norm_kernel<T, V, NV, 256, LAYER>, grid, 256, 0, st, p);
-    case 512: return launch_kernel(false, norm_kernel<T, V, NV, 512, LAYER>, grid, 512, 0, st, p);
-    default: return launch_kernel(false, norm_kernel<T, V, NV, 1024, LAYER>, grid, 1024, 0, st, p);
+    case 32: return launch_kernel(true, norm_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p);
+    case 128: return launch_kernel(true, norm_kernel<T, V, NV, 128, LAYER>, grid, 128, 0, st, p);
+    case 256: return launch_kernel(true, norm_kernel<T, V, NV, 256, LAYER>, grid, 256, 0, st, p);
+    case 512: return launch_kernel(true, norm_kernel<T, V, NV, 512, LAYER>, grid, 512, 0, st, p);
+    default: return launch_kernel(true, norm_kernel<T, V, NV, 1024, LAYER>, grid, 1024, 0, st, p);
   }
 }
 
@@ -435,8 +465,8 @@ cudaError_t norm_forward_of(const NormLaunch& p, cudaStream_t st) {
   const bool vec = vectors_ok(p, false);
   if (p.cols > kNormCols) {
     const dim3 grid((unsigned)std::min<uint64_t>(p.rows, (uint64_t)sm_count() * 2));
-    return vec ? launch_kernel(false, norm_wide_kernel<T, V, LAYER>, grid, 1024, 0, st, p)
-               : launch_kernel(false, norm_wide_kernel<T, 1, LAYER>, grid, 1024, 0, st, p);
+    return vec ? launch_kernel(true, norm_wide_kernel<T, V, LAYER>, grid, 1024, 0, st, p)
+               : launch_kernel(true, norm_wide_kernel<T, 1, LAYER>, grid, 1024, 0, st, p);
   }
   return vec ? norm_forward<T, V, 16 / V, LAYER>(p, st) : norm_forward<T, 1, 16, LAYER>(p, st);
 }
@@ -446,7 +476,7 @@ template <int V, int NV>
 uint32_t backward_ctas(const NormLaunch& p) {
   const int t = threads_for<V, NV>(p.cols);
   const uint64_t ctas = t == 32 ? (p.rows + 3) / 4 : p.rows;
-  return (uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * (t >= 512 ? 1 : t == 256 ? 2 : 4));
+  return (uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * (1024 / std::max(t, 128)));
 }
 
 constexpr uint32_t kWideParts = 64;
@@ -454,8 +484,8 @@ constexpr uint32_t kWideParts = 64;
 uint32_t backward_parts(const NormLaunch& p) {
   if (p.cols > kWideCols) return (uint32_t)std::min<uint64_t>(kWideParts, p.rows);
   const bool vec = vectors_ok(p, true);
-  if (!vec) return backward_ctas<1, 16>(p);
-  return p.dtype == MP_BF16 ? backward_ctas<8, 2>(p) : backward_ctas<4, 4>(p);
+  if (!vec) return backward_ctas<1, 8>(p);
+  return p.dtype == MP_BF16 ? backward_ctas<8, 1>(p) : backward_ctas<4, 2>(p);
 }
 
 template <typename T, int V, int NV, bool LAYER>
@@ -463,10 +493,11 @@ cudaError_t norm_backward(const NormLaunch& p, float* part, cudaStream_t st) {
   const int t = threads_for<V, NV>(p.cols);
   const dim3 grid(backward_ctas<V, NV>(p));
   switch (t) {
-    case 32: return launch_kernel(false, norm_backward_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p, part);
-    case 128: return launch_kernel(false, norm_backward_kernel<T, V, NV, 128, LAYER>, grid, 128, 0, st, p, part);
-    case 256: return launch_kernel(false, norm_backward_kernel<T, V, NV, 256, LAYER>, grid, 256, 0, st, p, part);
-    default: return launch_kernel(false, norm_backward_kernel<T, V, NV, 512, LAYER>, grid, 512, 0, st, p, part);
+    case 32: return launch_kernel(true, norm_backward_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p, part);
+    case 128: return launch_kernel(true, norm_backward_kernel<T, V, NV, 128, LAYER>, grid, 128, 0, st, p, part);
+    case 256: return launch_kernel(true, norm_backward_kernel<T, V, NV, 256, LAYER>, grid, 256, 0, st, p, part);
+    case 512: return launch_kernel(true, norm_backward_kernel<T, V, NV, 512, LAYER>, grid, 512, 0, st, p, part);
+    default: return launch_kernel(true, norm_backward_kernel<T, V, NV, 1024, LAYER>, grid, 1024, 0, st, p, part);
   }
 }
 
@@ -477,24 +508,24 @@ cudaError_t norm_backward_of(const NormLaunch& p, float* part, cudaStream_t st) 
   if (p.cols > kWideCols) {
     if (p.dx) {
       const dim3 grid((unsigned)std::min<uint64_t>(p.rows, (uint64_t)sm_count() * 2));
-      const cudaError_t e = vec ? launch_kernel(false, norm_backward_wide_kernel<T, V, LAYER>, grid, 1024, 0, st, p)
-                                : launch_kernel(false, norm_backward_wide_kernel<T, 1, LAYER>, grid, 1024, 0, st, p);
+      const cudaError_t e = vec ? launch_kernel(true, norm_backward_wide_kernel<T, V, LAYER>, grid, 1024, 0, st, p)
+                                : launch_kernel(true, norm_backward_wide_kernel<T, 1, LAYER>, grid, 1024, 0, st, p);
       if (e != cudaSuccess) return e;
     }
     if (!part) return cudaSuccess;
     const uint32_t n = backward_parts(p);
     const dim3 grid((p.cols + 255u) / 256u, n);
-    return launch_kernel(p.dx != nullptr, norm_weight_sums_kernel<T, LAYER>, grid, 256, 0, st, p, part,
+    return launch_kernel(true, norm_weight_sums_kernel<T, LAYER>, grid, 256, 0, st, p, part,
                          (p.rows + n - 1) / n);
   }
-  return vec ? norm_backward<T, V, 16 / V, LAYER>(p, part, st) : norm_backward<T, 1, 16, LAYER>(p, part, st);
+  return vec ? norm_backward<T, V, 8 / V, LAYER>(p, part, st) : norm_backward<T, 1, 8, LAYER>(p, part, st);
 }
 
 template <typename T>
 cudaError_t column_sums(const float* part, uint32_t n_part, uint64_t stride, uint32_t cols, void* a, void* b,
                         cudaStream_t st) {
   const dim3 grid((cols + 31u) / 32u, b ? 2 : 1);
-  return launch_kernel(true, column_sums_kernel<T>, grid, 256, 0, st, part, n_part, stride, cols, static_cast<T*>(a),
+  return launch_kernel(true, column_sums_kernel<T>, grid, 1024, 0, st, part, n_part, stride, cols, static_cast<T*>(a),
                        static_cast<T*>(b));
 }
 

@@ -60,6 +60,12 @@ __device__ __forceinline__ void umma_commit(uint64_t* bar) {
         : "memory");
 }
 
+// A kernel that takes tensor memory and may start before the one ahead of it has ended (launch_kernel) waits for
+// that end first, takes its memory, and only then lets the next one start: two kernels that wait for one another, one
+// for an end and one for columns, cannot come about, whatever kernels run ahead and behind.
+__device__ __forceinline__ void kernel_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void kernel_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // columns of tensor memory (a power of two, 32 at least) for the CTA or the pair; a whole warp calls it
 template <int CG>
 __device__ __forceinline__ void tmem_alloc(uint32_t* where, uint32_t cols) {
@@ -132,9 +138,12 @@ __device__ __forceinline__ uint32_t cluster_map(uint32_t a, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
   return r;
 }
-__device__ __forceinline__ float cluster_load(uint32_t a) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+__device__ __forceinline__ float4 cluster_load4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(a)
+               : "memory");
   return v;
 }
 __device__ __forceinline__ void cluster_arrive(uint32_t bar) {

@@ -684,7 +684,7 @@ def test_failed_scratch_and_calls_after_it(mp):
             continue
         break
     mp.mp_debug_inject_fault(mp.MP_FAULT_ALLOC, 0)
-    assert n >= 3
+    assert n >= 2
     got = mp.mp_linear_backward(dy, c["x"], c["w"], bias=True)
     assert all(torch.equal(a, b) for a, b in zip(got[:3], want[:3]))
     mp.mp_layer_status()
