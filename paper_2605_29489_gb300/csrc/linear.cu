@@ -31,7 +31,7 @@ namespace {
 
 // ---- the epilogue -------------------------------------------------------------------------------
 
-// act(z) and act'(z).  FAST: bf16 results, where the fast exponential's 2 ulp do not show.
+// act(z).  FAST: bf16 results, where the fast exponential's 2 ulp do not show.
 template <bool FAST>
 __device__ __forceinline__ float sigmoid(float z) {
   return FAST ? __fdividef(1.0f, 1.0f + __expf(-z)) : 1.0f / (1.0f + expf(-z));
@@ -47,20 +47,31 @@ __device__ __forceinline__ float act_of(float z) {
   if constexpr (ACT == MP_ACT_GELU_TANH) return 0.5f * z * (1.0f + tanhf(kRoot2Pi * fmaf(kTanhCubic * z * z, z, z)));
   return z;
 }
+// act(z) in a and act'(z) in g: they share what costs most
 template <int ACT, bool FAST>
-__device__ __forceinline__ float act_grad(float z) {
-  if constexpr (ACT == MP_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+__device__ __forceinline__ void act_both(float z, float& a, float& g) {
+  a = z;
+  g = 1.0f;
+  if constexpr (ACT == MP_ACT_RELU) {
+    a = act_of<ACT, FAST>(z);
+    g = z > 0.0f ? 1.0f : 0.0f;
+  }
   if constexpr (ACT == MP_ACT_SILU) {
     const float s = sigmoid<FAST>(z);
-    return s * fmaf(z, 1.0f - s, 1.0f);
+    a = z * s;
+    g = s * fmaf(z, 1.0f - s, 1.0f);
   }
-  if constexpr (ACT == MP_ACT_GELU) return fmaf(z, kInvRoot2Pi * expf(-0.5f * z * z), 0.5f * (1.0f + erff(z * kRootHalf)));
+  if constexpr (ACT == MP_ACT_GELU) {
+    const float s = 0.5f * (1.0f + erff(z * kRootHalf));
+    a = z * s;
+    g = fmaf(z, kInvRoot2Pi * expf(-0.5f * z * z), s);
+  }
   if constexpr (ACT == MP_ACT_GELU_TANH) {
-    const float t = tanhf(kRoot2Pi * fmaf(kTanhCubic * z * z, z, z));
+    const float t = tanhf(kRoot2Pi * fmaf(kTanhCubic * z * z, z, z)), s = 0.5f * (1.0f + t);
     const float c = fminf(fmaxf(z, -16.0f), 16.0f);  // t is +-1 from there on: no 0 * infinity
-    return fmaf(0.5f * c * (1.0f - t * t), kRoot2Pi * fmaf(3.0f * kTanhCubic * c, c, 1.0f), 0.5f * (1.0f + t));
+    a = z * s;
+    g = fmaf(0.5f * c * (1.0f - t * t), kRoot2Pi * fmaf(3.0f * kTanhCubic * c, c, 1.0f), s);
   }
-  return 1.0f;
 }
 
 template <bool FAST, int N>
@@ -123,22 +134,23 @@ __device__ __forceinline__ void epi_quad(const Epi<T>& e, uint32_t r, uint32_t c
       if (c + k < e.cols) epi_one(e, r, c + k, v[k]);
     return;
   }
-  Pack<T, 4> q, m, s;
+  Pack<T, 4> m, s;
   if (e.mul) m = *reinterpret_cast<const Pack<T, 4>*>(e.mul + r * e.ldmul + c);
   if (e.res) s = *reinterpret_cast<const Pack<T, 4>*>(e.res + r * e.ldres + c);
-  if (e.pre) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) q.e[k] = Elem<T>::store(v[k]);
-    *reinterpret_cast<Pack<T, 4>*>(e.pre + r * e.ldpre + c) = q;
-  }
+  if (e.pre) *reinterpret_cast<Pack<T, 4>*>(e.pre + r * e.ldpre + c) = pack<T, 4>(v);
   act_all<FAST, 4>(e.act, v);
+  float u[4];
+  if (e.mul) {
+    unpack(m, u);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (e.mul) v[k] *= Elem<T>::load(m.e[k]);
-    if (e.res) v[k] += Elem<T>::load(s.e[k]);
-    q.e[k] = Elem<T>::store(v[k]);
+    for (int k = 0; k < 4; ++k) v[k] *= u[k];
   }
-  *reinterpret_cast<Pack<T, 4>*>(e.y + r * e.ldy + c) = q;
+  if (e.res) {
+    unpack(s, u);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += u[k];
+  }
+  *reinterpret_cast<Pack<T, 4>*>(e.y + r * e.ldy + c) = pack<T, 4>(v);
 }
 
 // N consecutive columns of a row, from c on (a multiple of N), of which those below e.cols exist
@@ -158,47 +170,38 @@ __device__ __forceinline__ void epi_run(const Epi<T>& e, uint32_t r, uint32_t c,
       }
     return;
   }
+  float u[V];
   if (e.bias) {
 #pragma unroll
     for (int j = 0; j < N; j += V) {
-      const Pack<T, V> q = load_pack<T, V>(e.bias + c + j);
+      unpack(load_pack<T, V>(e.bias + c + j), u);
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[j + k] += Elem<T>::load(q.e[k]);
+      for (int k = 0; k < V; ++k) v[j + k] += u[k];
     }
   }
   if (e.pre) {
 #pragma unroll
-    for (int j = 0; j < N; j += V) {
-      Pack<T, V> q;
-#pragma unroll
-      for (int k = 0; k < V; ++k) q.e[k] = Elem<T>::store(v[j + k]);
-      store_pack<T, V>(e.pre + r * e.ldpre + c + j, q);
-    }
+    for (int j = 0; j < N; j += V) store_pack<T, V>(e.pre + r * e.ldpre + c + j, pack<T, V>(v + j));
   }
   act_all<FAST, N>(e.act, v);
   if (e.mul) {
 #pragma unroll
     for (int j = 0; j < N; j += V) {
-      const Pack<T, V> q = load_pack<T, V>(e.mul + r * e.ldmul + c + j);
+      unpack(load_pack<T, V>(e.mul + r * e.ldmul + c + j), u);
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[j + k] *= Elem<T>::load(q.e[k]);
+      for (int k = 0; k < V; ++k) v[j + k] *= u[k];
     }
   }
   if (e.res) {
 #pragma unroll
     for (int j = 0; j < N; j += V) {
-      const Pack<T, V> q = load_pack<T, V>(e.res + r * e.ldres + c + j);
+      unpack(load_pack<T, V>(e.res + r * e.ldres + c + j), u);
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[j + k] += Elem<T>::load(q.e[k]);
+      for (int k = 0; k < V; ++k) v[j + k] += u[k];
     }
   }
 #pragma unroll
-  for (int j = 0; j < N; j += V) {
-    Pack<T, V> q;
-#pragma unroll
-    for (int k = 0; k < V; ++k) q.e[k] = Elem<T>::store(v[j + k]);
-    store_pack<T, V>(e.y + r * e.ldy + c + j, q);
-  }
+  for (int j = 0; j < N; j += V) store_pack<T, V>(e.y + r * e.ldy + c + j, pack<T, V>(v + j));
 }
 
 // ---- tensor-core products -----------------------------------------------------------------------
@@ -659,23 +662,25 @@ __global__ void __launch_bounds__(256) dz_kernel(const DzArgs<T> p) {
   if (c < p.cols) {
 #pragma unroll 2
     for (uint64_t r = q0 + warp; r < q1; r += 8) {
-      const Pack<T, V> dy = load_pack<T, V>(p.dy + r * p.lddy + c);
-      Pack<T, V> z, m, o, om;
-      if (p.pre) z = load_pack<T, V>(p.pre + r * p.ldpre + c);
-      if (p.mul) m = load_pack<T, V>(p.mul + r * p.ldmul + c);
+      const Pack<T, V> dq = load_pack<T, V>(p.dy + r * p.lddy + c);
+      Pack<T, V> zq, mq;
+      if (p.pre) zq = load_pack<T, V>(p.pre + r * p.ldpre + c);
+      if (p.mul) mq = load_pack<T, V>(p.mul + r * p.ldmul + c);
+      float d[V], z[V] = {}, m[V], om[V];
+      unpack(dq, d);
+      if (p.pre) unpack(zq, z);
+      if (p.mul) unpack(mq, m);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float d = Elem<T>::load(dy.e[k]);
-        const float zk = p.pre ? Elem<T>::load(z.e[k]) : 0.0f;
-        float g = d;
-        if (ACT != MP_ACT_NONE) g *= act_grad<ACT, FAST>(zk);
-        if (p.mul) g *= Elem<T>::load(m.e[k]);
-        if (p.dmul) om.e[k] = Elem<T>::store(d * act_of<ACT, FAST>(zk));
-        o.e[k] = Elem<T>::store(g);
-        s[k] += g;
+        float a, g;
+        act_both<ACT, FAST>(z[k], a, g);
+        om[k] = d[k] * a;
+        if (ACT != MP_ACT_NONE) d[k] *= g;
+        if (p.mul) d[k] *= m[k];
+        s[k] += d[k];
       }
-      if (p.dz) store_pack<T, V>(p.dz + r * p.lddz + c, o);
-      if (p.dmul) store_pack<T, V>(p.dmul + r * p.lddmul + c, om);
+      if (p.dz) store_pack<T, V>(p.dz + r * p.lddz + c, pack<T, V>(d));
+      if (p.dmul) store_pack<T, V>(p.dmul + r * p.lddmul + c, pack<T, V>(om));
     }
   }
   if (!p.part) return;
@@ -817,7 +822,8 @@ template <int BN, bool AT, bool BT>
 cudaError_t launch_split(const CUtensorMap& ma, const CUtensorMap& mb, const Epi<bf16>& e, uint32_t kb, unsigned split,
                          int stages, const Wait& w, cudaStream_t st) {
   const uint32_t tiles_r = (e.rows + BN - 1) / BN, tiles_c = (e.cols + 127u) / 128u;
-  const size_t smem = (size_t)stages * (128 * 128 + BN * 128) + 1024;
+  // the stages, and in their place the sums at the end ([BN][128] fp32)
+  const size_t smem = std::max((size_t)stages * (128 * 128 + BN * 128), (size_t)BN * 512) + 1024;
   return launch_cluster(split_kernel<BN, AT, BT>, tiles_r * tiles_c * split, kGemmThreads, split, smem, st, ma, mb, e, kb, tiles_r,
                         stages, w);
 }
@@ -865,10 +871,18 @@ mp_status gemm_bf16(const GemmLaunch& g, cudaStream_t st) {
                 : launch_big<2, false, false>(ma, mb, e, kb, w, st);
   } else {
     const uint64_t tiles = ((g.e.rows + bn - 1) / bn) * ((g.e.cols + 127) / 128);
-    unsigned split = 1;
-    while (split < 8 && tiles * split * 2 <= sms * 2 && kb >= 4 * split) split *= 2;
+    // As many CTAs as share a tile while three to an SM hold them all and each has two stages at least, and as many
+    // stages as shared memory holds then (with a tenth of the SMs' places to spare: clusters do not fill every one).
+    // One row, 4096 -> 14336, 112 tiles: 26.8 us unsplit, 23.0 with two CTAs of 5 stages, 21.9 with four of 3, 29 with
+    // four of 4 stages, which do not all fit; 24 rows, 14336 -> 4096, 32 tiles: 83 us unsplit, 25.1 with eight of 5.
     const int stage = 128 * 128 + bn * 128;
-    const int stages = std::min(6, 100 * 1024 / stage);
+    auto stages_with = [&](uint64_t ctas) {
+      const uint64_t per_sm = std::max<uint64_t>(1, std::min<uint64_t>(4, (ctas * 11 + sms * 10 - 1) / (sms * 10)));
+      return (int)std::min<uint64_t>(6, (228 * 1024 / per_sm - 2560) / stage);
+    };
+    unsigned split = 1;
+    while (split < 8 && tiles * split * 2 <= sms * 3 && kb >= 4 * split && stages_with(tiles * split * 2) >= 2) split *= 2;
+    const int stages = std::max(2, stages_with(tiles * split));
     r = g.a_t ? launch_split_of<true, true>(bn, mb, ma, e, kb, split, stages, w, st)
         : g.b_t ? launch_split_of<true, false>(bn, mb, ma, e, kb, split, stages, w, st)
                 : launch_split_of<false, false>(bn, mb, ma, e, kb, split, stages, w, st);

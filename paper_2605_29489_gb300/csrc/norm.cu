@@ -29,24 +29,26 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// sums of two values over the ROWT threads of a row; red: two sets of a pair per warp of the CTA, taken in turn (turn
-// counts the calls), so that one barrier is enough.  Every thread gets the same bits: with more than one warp each adds
-// the warps' sums in the same order.
-template <int ROWT, int WARPS>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2 (*red)[WARPS], uint32_t& turn) {
+// sums over the ROWT threads of a row, of a and, with TWO, of b; red: two sets of a pair per warp of the CTA, taken in
+// turn (turn counts the calls), so that one barrier is enough.  Every thread gets the same bits: the warps' sums go
+// through the same tree in each warp.
+template <int ROWT, bool TWO, int WARPS>
+__device__ __forceinline__ float2 row_sum(float a, float b, float2 (*red)[WARPS], uint32_t& turn) {
   a = warp_sum(a);
-  b = warp_sum(b);
+  if (TWO) b = warp_sum(b);
   if constexpr (ROWT > 32) {
     constexpr int W = ROWT / 32;
-    const int warp = threadIdx.x >> 5, first = (threadIdx.x / ROWT) * W;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = (threadIdx.x / ROWT) * W;
     float2* set = red[turn++ & 1u];
-    if ((threadIdx.x & 31) == 0) set[warp] = make_float2(a, b);
+    if (lane == 0) set[warp] = make_float2(a, b);
     __syncthreads();
-    a = b = 0.0f;
+    const float2 v = set[first + lane % W];
+    a = v.x;
+    b = v.y;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      a += set[first + w].x;
-      b += set[first + w].y;
+    for (int o = W / 2; o > 0; o >>= 1) {
+      a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+      if (TWO) b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
     }
   }
   return make_float2(a, b);
@@ -59,9 +61,11 @@ constexpr int cta_of() {
 }
 
 // The next row's loads are on their way while this one's sums are taken: the time is that of the bytes, not of the
-// steps from the first load of a row to its last store.
+// steps from the first load of a row to its last store.  A row stays as it is stored (4 registers for 8 bf16) and is
+// taken apart again where it is used, so that kForward threads fit an SM.
+constexpr int kForward = 1024;
 template <typename T, int V, int NV, int ROWT, bool LAYER>
-__global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_kernel(const NormLaunch p) {
+__global__ void __launch_bounds__(cta_of<ROWT>(), kForward / cta_of<ROWT>()) norm_kernel(const NormLaunch p) {
   kernel_begin();
   constexpr int kRows = cta_of<ROWT>() / ROWT;
   __shared__ float2 red[2][cta_of<ROWT>() / 32];
@@ -71,47 +75,47 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_kernel(const NormLaunc
   const T* b = static_cast<const T*>(p.bias);
   const float inv = 1.0f / (float)p.cols;
   const uint64_t step = (uint64_t)gridDim.x * kRows;
-  Pack<T, V> q[NV];
+  constexpr bool kAhead = !(LAYER && V == 1 && sizeof(T) == 2);  // else the next row does not fit the registers
+  auto place = [&](int k) { return (uint32_t)(k * ROWT + lane) * V; };
+  Pack<T, V> next[NV];
   auto fetch = [&](uint64_t r) {
     const T* x = static_cast<const T*>(p.x) + r * p.ldx;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
-      if (c < p.cols) q[k] = load_pack<T, V>(x + c);
-    }
+    for (int k = 0; k < NV; ++k)
+      if (place(k) < p.cols) next[k] = load_pack<T, V>(x + place(k));
   };
   uint64_t r0 = (uint64_t)blockIdx.x * kRows;
-  if (r0 + threadIdx.x / ROWT < p.rows) fetch(r0 + threadIdx.x / ROWT);
+  if (kAhead && r0 + threadIdx.x / ROWT < p.rows) fetch(r0 + threadIdx.x / ROWT);
   // the rows of a CTA go on together (its threads meet at the sums): r0 is the same for all of them
   for (; r0 < p.rows; r0 += step) {
     const uint64_t r = r0 + threadIdx.x / ROWT;
-    float v[NV * V];
+    Pack<T, V> q[NV];
+    float v[V];
     float s = 0.0f;
+    if (!kAhead && r < p.rows) fetch(r);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+    for (int k = 0; k < NV; ++k) q[k] = next[k];
+    if (kAhead && r + step < p.rows) fetch(r + step);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        v[k * V + e] = c < p.cols ? Elem<T>::load(q[k].e[e]) : 0.0f;
-        s = LAYER ? s + v[k * V + e] : fmaf(v[k * V + e], v[k * V + e], s);
+    for (int k = 0; k < NV; ++k)
+      if (place(k) < p.cols) {
+        unpack(q[k], v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s = LAYER ? s + v[e] : fmaf(v[e], v[e], s);
       }
-    }
-    if (r + step < p.rows) fetch(r + step);
     float mu = 0.0f;
     if (LAYER) {
-      mu = row_sum2<ROWT>(s, 0.0f, red, turn).x * inv;
+      mu = row_sum<ROWT, false>(s, 0.0f, red, turn).x * inv;
       s = 0.0f;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
+      for (int k = 0; k < NV; ++k)
+        if (place(k) < p.cols) {
+          unpack(q[k], v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          v[k * V + e] -= mu;
-          if (c < p.cols) s = fmaf(v[k * V + e], v[k * V + e], s);
+          for (int e = 0; e < V; ++e) s = fmaf(v[e] - mu, v[e] - mu, s);
         }
-      }
     }
-    const float var = row_sum2<ROWT>(s, 0.0f, red, turn).x * inv;
+    const float var = row_sum<ROWT, false>(s, 0.0f, red, turn).x * inv;
     const float rstd = 1.0f / sqrtf(var + p.eps);
     if (r < p.rows) {
       if (lane == 0) {
@@ -120,22 +124,24 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), 1) norm_kernel(const NormLaunc
       }
       T* y = static_cast<T*>(p.y) + r * p.ldy;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
-        if (c < p.cols) {
-          Pack<T, V> o, wq, bq;
-          if (w) wq = load_pack<T, V>(w + c);
-          if (b) bq = load_pack<T, V>(b + c);
+      for (int k = 0; k < NV; ++k)
+        if (place(k) < p.cols) {
+          float u[V];
+          unpack(q[k], v);
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float t = v[k * V + e] * rstd;
-            if (w) t *= Elem<T>::load(wq.e[e]);
-            if (b) t += Elem<T>::load(bq.e[e]);
-            o.e[e] = Elem<T>::store(t);
+          for (int e = 0; e < V; ++e) v[e] = (LAYER ? v[e] - mu : v[e]) * rstd;
+          if (w) {
+            unpack(load_pack<T, V>(w + place(k)), u);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] *= u[e];
           }
-          store_pack<T, V>(y + c, o);
+          if (b) {
+            unpack(load_pack<T, V>(b + place(k)), u);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] += u[e];
+          }
+          store_pack<T, V>(y + place(k), pack<T, V>(v));
         }
-      }
     }
   }
 }
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) 
 #pragma unroll
         for (int e = 0; e < V; ++e) s += Elem<T>::load(q.e[e]);
       }
-      mu = row_sum2<1024>(s, 0.0f, red, turn).x * inv;
+      mu = row_sum<1024, false>(s, 0.0f, red, turn).x * inv;
       s = 0.0f;
     }
     for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
@@ -169,7 +175,7 @@ __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) 
         s = fmaf(t, t, s);
       }
     }
-    const float rstd = 1.0f / sqrtf(row_sum2<1024>(s, 0.0f, red, turn).x * inv + p.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<1024, false>(s, 0.0f, red, turn).x * inv + p.eps);
     if (threadIdx.x == 0) {
       if (p.rstd) p.rstd[r] = rstd;
       if (LAYER && p.mean) p.mean[r] = mu;
@@ -192,35 +198,47 @@ __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) 
   }
 }
 
-// dx of the rows of a CTA and its sums for dw (part [2 * cta]) and db (part [2 * cta + 1]); sums: whether those
-// are wanted.  A thread has 8 columns (NV * V): x, dy and the next row's stay as they are stored, the sums take two
-// registers a column, and 1024 threads fit an SM.
-template <typename T, int V, int NV, int ROWT, bool LAYER>
-__global__ void __launch_bounds__(cta_of<ROWT>(), 1024 / cta_of<ROWT>()) norm_backward_kernel(const NormLaunch p, float* part) {
+// The backward pass's threads to an SM, and the columns of one: 16 of bf16 (what a row costs besides its elements is
+// then half of what it is with 8), 8 of fp32, whose elements take twice the registers.
+template <typename T, int V>
+constexpr int backward_threads() {
+  return sizeof(T) == 2 && V > 1 ? 512 : 1024;
+}
+template <typename T, int V>
+constexpr int backward_vecs() {
+  return 8192 / backward_threads<T, V>() / V;
+}
+
+// dx of the rows of a CTA and its sums for dw (part [2 * cta]) and db (part [2 * cta + 1]).  The next row's loads are on
+// their way while this one's sums are taken.
+template <typename T, int V, int ROWT, bool LAYER>
+__global__ void __launch_bounds__(cta_of<ROWT>(), (ROWT == 32 ? 3 : 4) * backward_threads<T, V>() / 4 / cta_of<ROWT>())
+    norm_backward_kernel(const NormLaunch p, float* part) {
   kernel_begin();
-  constexpr int kRows = cta_of<ROWT>() / ROWT;
+  constexpr int NV = backward_vecs<T, V>(), kRows = cta_of<ROWT>() / ROWT;
+  constexpr bool kAddAhead = backward_threads<T, V>() == 512;  // else the registers do not hold the next row's
   __shared__ float2 red[2][cta_of<ROWT>() / 32];
   uint32_t turn = 0;
   const int lane = threadIdx.x % ROWT;
   const T* w = static_cast<const T*>(p.weight);
   const float inv = 1.0f / (float)p.cols;
   const uint64_t step = (uint64_t)gridDim.x * kRows;
+  auto place = [&](int k) { return (uint32_t)(k * ROWT + lane) * V; };
   float aw[NV * V] = {}, ab[NV * V] = {};
-  Pack<T, V> xn[NV], dn[NV];  // the next row
+  Pack<T, V> xn[NV], dn[NV], an[NV];  // the next row
   float mun = 0.0f, rstdn = 0.0f;
   auto fetch = [&](uint64_t r) {
     const T* x = static_cast<const T*>(p.x) + r * p.ldx;
     const T* dy = static_cast<const T*>(p.dy) + r * p.lddy;
-    mun = LAYER ? p.mean[r] : 0.0f;
+    if (LAYER) mun = p.mean[r];
     rstdn = p.rstd[r];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
-      if (c < p.cols) {
-        xn[k] = load_pack<T, V>(x + c);
-        dn[k] = load_pack<T, V>(dy + c);
+    for (int k = 0; k < NV; ++k)
+      if (place(k) < p.cols) {
+        xn[k] = load_pack<T, V>(x + place(k));
+        dn[k] = load_pack<T, V>(dy + place(k));
+        if (kAddAhead && p.add) an[k] = load_pack<T, V>(static_cast<const T*>(p.add) + r * p.ldadd + place(k));
       }
-    }
   };
   uint64_t r0 = (uint64_t)blockIdx.x * kRows;
   if (r0 + threadIdx.x / ROWT < p.rows) fetch(r0 + threadIdx.x / ROWT);
@@ -228,61 +246,47 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), 1024 / cta_of<ROWT>()) norm_ba
     const uint64_t r = r0 + threadIdx.x / ROWT;
     const bool live = r < p.rows;
     const float mu = mun, rstd = rstdn;
-    Pack<T, V> xq[NV], dq[NV], aq[NV];
-    const T* add = p.add && live ? static_cast<const T*>(p.add) + r * p.ldadd : nullptr;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
-      xq[k] = xn[k];
-      dq[k] = dn[k];
-      if (add && c < p.cols) aq[k] = load_pack<T, V>(add + c);
-    }
-    if (r + step < p.rows) fetch(r + step);
+    float h[NV * V], g[NV * V], u[V];
     float s1 = 0.0f, s2 = 0.0f;
+    Pack<T, V> aq[NV];
     if (live) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
-        if (c < p.cols) {
-          Pack<T, V> wq;
-          if (w) wq = load_pack<T, V>(w + c);
+      for (int k = 0; k < NV; ++k)
+        if (place(k) < p.cols) {
+          float *hk = h + k * V, *gk = g + k * V;
+          unpack(xn[k], hk);
+          unpack(dn[k], gk);
+          if (kAddAhead) aq[k] = an[k];
+          if (w) unpack(load_pack<T, V>(w + place(k)), u);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
-            const float d = Elem<T>::load(dq[k].e[e]);
-            const float h = (Elem<T>::load(xq[k].e[e]) - mu) * rstd;
-            const float g = w ? d * Elem<T>::load(wq.e[e]) : d;
-            s1 = fmaf(g, h, s1);
-            if (LAYER) s2 += g;
-            aw[k * V + e] = fmaf(d, h, aw[k * V + e]);
-            if (LAYER) ab[k * V + e] += d;
+            hk[e] = (LAYER ? hk[e] - mu : hk[e]) * rstd;
+            aw[k * V + e] = fmaf(gk[e], hk[e], aw[k * V + e]);
+            if (LAYER) ab[k * V + e] += gk[e];
+            if (w) gk[e] *= u[e];
+            s1 = fmaf(gk[e], hk[e], s1);
+            if (LAYER) s2 += gk[e];
           }
         }
-      }
     }
+    if (r + step < p.rows) fetch(r + step);
     if (!p.dx) continue;
-    const float2 m = row_sum2<ROWT>(s1, s2, red, turn);
+    const float2 m = row_sum<ROWT, LAYER>(s1, s2, red, turn);
     const float m1 = m.x * inv, m2 = m.y * inv;
     if (live) {
       T* dx = static_cast<T*>(p.dx) + r * p.lddx;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const uint32_t c = (uint32_t)(k * ROWT + lane) * V;
-        if (c < p.cols) {
-          Pack<T, V> o, wq;
-          if (w) wq = load_pack<T, V>(w + c);
+      for (int k = 0; k < NV; ++k)
+        if (place(k) < p.cols) {
+          float* gk = g + k * V;
+          if (p.add) unpack(kAddAhead ? aq[k] : load_pack<T, V>(static_cast<const T*>(p.add) + r * p.ldadd + place(k)), u);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
-            const float d = Elem<T>::load(dq[k].e[e]);
-            const float h = (Elem<T>::load(xq[k].e[e]) - mu) * rstd;
-            float t = w ? d * Elem<T>::load(wq.e[e]) : d;
-            if (LAYER) t -= m2;
-            t = (t - h * m1) * rstd;
-            if (add) t += Elem<T>::load(aq[k].e[e]);
-            o.e[e] = Elem<T>::store(t);
+            gk[e] = fmaf(-h[k * V + e], m1, LAYER ? gk[e] - m2 : gk[e]) * rstd;
+            if (p.add) gk[e] += u[e];
           }
-          store_pack<T, V>(dx + c, o);
+          store_pack<T, V>(dx + place(k), pack<T, V>(gk));
         }
-      }
     }
   }
   if (!part) return;
@@ -348,7 +352,7 @@ __global__ void __launch_bounds__(1024, 1) norm_backward_wide_kernel(const NormL
         s2 += g;
       }
     }
-    const float2 m = row_sum2<1024>(s1, s2, red, turn);
+    const float2 m = row_sum<1024, true>(s1, s2, red, turn);
     const float m1 = m.x * inv, m2 = LAYER ? m.y * inv : 0.0f;
     T* dx = static_cast<T*>(p.dx) + r * p.lddx;
     for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
@@ -425,6 +429,9 @@ bool vectors_ok(const NormLaunch& p, bool backward) {
   const size_t es = p.dtype == MP_BF16 ? 2 : 4;
   if ((p.cols * es) % 16 != 0 || !row16(p.x, p.ldx, es) || !row16(p.weight, 0, es)) return false;
   if (!backward) return row16(p.y, p.ldy, es) && row16(p.bias, 0, es);
+  // the backward pass of an fp32 layer norm goes element by element, a warp's access being 128 bytes all the same: with
+  // vectors its registers do not hold a row, the next one and two sums per column
+  if (p.dtype == MP_F32 && p.layer && p.cols <= kWideCols) return false;
   return row16(p.dy, p.lddy, es) && row16(p.add, p.ldadd, es) && row16(p.dx, p.lddx, es);
 }
 
@@ -448,7 +455,7 @@ template <typename T, int V, int NV, bool LAYER>
 cudaError_t norm_forward(const NormLaunch& p, cudaStream_t st) {
   const int t = threads_for<V, NV>(p.cols);
   const uint64_t ctas = t == 32 ? (p.rows + 3) / 4 : p.rows;
-  const uint64_t most = (uint64_t)sm_count() * (2048 / std::max(t, 128));
+  const uint64_t most = (uint64_t)sm_count() * (kForward / std::max(t, 128));
   const dim3 grid((unsigned)std::min(ctas, most));
   switch (t) {
     case 32: return launch_kernel(true, norm_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p);
@@ -472,11 +479,11 @@ cudaError_t norm_forward_of(const NormLaunch& p, cudaStream_t st) {
 }
 
 // the CTAs of the backward pass: sums of fewer CTAs are less to write and read again
-template <int V, int NV>
+template <typename T, int V>
 uint32_t backward_ctas(const NormLaunch& p) {
-  const int t = threads_for<V, NV>(p.cols);
+  const int t = threads_for<V, backward_vecs<T, V>()>(p.cols);
   const uint64_t ctas = t == 32 ? (p.rows + 3) / 4 : p.rows;
-  return (uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * (1024 / std::max(t, 128)));
+  return (uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * ((t == 32 ? 3 : 4) * backward_threads<T, V>() / 4 / std::max(t, 128)));
 }
 
 constexpr uint32_t kWideParts = 64;
@@ -484,20 +491,22 @@ constexpr uint32_t kWideParts = 64;
 uint32_t backward_parts(const NormLaunch& p) {
   if (p.cols > kWideCols) return (uint32_t)std::min<uint64_t>(kWideParts, p.rows);
   const bool vec = vectors_ok(p, true);
-  if (!vec) return backward_ctas<1, 8>(p);
-  return p.dtype == MP_BF16 ? backward_ctas<8, 1>(p) : backward_ctas<4, 2>(p);
+  if (p.dtype == MP_BF16) return vec ? backward_ctas<__nv_bfloat16, 8>(p) : backward_ctas<__nv_bfloat16, 1>(p);
+  return vec ? backward_ctas<float, 4>(p) : backward_ctas<float, 1>(p);
 }
 
-template <typename T, int V, int NV, bool LAYER>
-cudaError_t norm_backward(const NormLaunch& p, float* part, cudaStream_t st) {
-  const int t = threads_for<V, NV>(p.cols);
-  const dim3 grid(backward_ctas<V, NV>(p));
-  switch (t) {
-    case 32: return launch_kernel(true, norm_backward_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p, part);
-    case 128: return launch_kernel(true, norm_backward_kernel<T, V, NV, 128, LAYER>, grid, 128, 0, st, p, part);
-    case 256: return launch_kernel(true, norm_backward_kernel<T, V, NV, 256, LAYER>, grid, 256, 0, st, p, part);
-    case 512: return launch_kernel(true, norm_backward_kernel<T, V, NV, 512, LAYER>, grid, 512, 0, st, p, part);
-    default: return launch_kernel(true, norm_backward_kernel<T, V, NV, 1024, LAYER>, grid, 1024, 0, st, p, part);
+template <typename T, int V, bool LAYER>
+cudaError_t norm_backward_rows(const NormLaunch& p, float* part, cudaStream_t st) {
+  const dim3 grid(backward_ctas<T, V>(p));
+  switch (threads_for<V, backward_vecs<T, V>()>(p.cols)) {
+    case 32: return launch_kernel(true, norm_backward_kernel<T, V, 32, LAYER>, grid, 128, 0, st, p, part);
+    case 128: return launch_kernel(true, norm_backward_kernel<T, V, 128, LAYER>, grid, 128, 0, st, p, part);
+    case 256: return launch_kernel(true, norm_backward_kernel<T, V, 256, LAYER>, grid, 256, 0, st, p, part);
+    case 512: return launch_kernel(true, norm_backward_kernel<T, V, 512, LAYER>, grid, 512, 0, st, p, part);
+    default:
+      if constexpr (backward_threads<T, V>() == 1024)
+        return launch_kernel(true, norm_backward_kernel<T, V, 1024, LAYER>, grid, 1024, 0, st, p, part);
+      return cudaErrorInvalidValue;  // rows of up to kWideCols take 512 threads
   }
 }
 
@@ -518,7 +527,9 @@ cudaError_t norm_backward_of(const NormLaunch& p, float* part, cudaStream_t st) 
     return launch_kernel(true, norm_weight_sums_kernel<T, LAYER>, grid, 256, 0, st, p, part,
                          (p.rows + n - 1) / n);
   }
-  return vec ? norm_backward<T, V, 8 / V, LAYER>(p, part, st) : norm_backward<T, 1, 8, LAYER>(p, part, st);
+  if constexpr (!(LAYER && sizeof(T) == 4))
+    if (vec) return norm_backward_rows<T, V, LAYER>(p, part, st);
+  return norm_backward_rows<T, 1, LAYER>(p, part, st);
 }
 
 template <typename T>
