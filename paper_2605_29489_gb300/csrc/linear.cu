@@ -235,20 +235,19 @@ __device__ __forceinline__ void give_up(volatile int* abort, const Wait& w) {
   atomicOr_system(w.err, kErrTimeout);
 }
 
-// the rounds of a bounded wait on an mbarrier that threads of another CTA arrive on
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort, uint32_t limit) {
+// a warp's bounded wait on an mbarrier that threads of another CTA arrive on
+__device__ __forceinline__ bool warp_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort, uint32_t limit) {
+  uint32_t ok = 0;
   for (uint32_t k = 0; k < limit; ++k) {
-    uint32_t ok;
     asm volatile(
         "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, "
         "p;\n}\n"
         : "=r"(ok)
         : "r"(su32(bar)), "r"(parity)
         : "memory");
-    if (ok) return true;
-    if ((k & 15u) == 15u && *abort) return false;
+    if (ok || ((k & 15u) == 15u && *abort)) break;
   }
-  return false;
+  return __all_sync(0xFFFFFFFFu, ok != 0);
 }
 
 // Few rows.  out[r, c]: c (features, the lanes of tensor memory) from operand a, r from operand b.  A cluster makes one
@@ -265,7 +264,7 @@ __global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_consta
   __shared__ uint32_t tmem_at;
   __shared__ volatile int abort;
   const uint32_t smem = (su32(raw) + 1023u) & ~1023u;
-  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
   uint32_t split, rank = cluster_rank();
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(split));
   const uint32_t tile = blockIdx.x / split;
@@ -289,40 +288,45 @@ __global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_consta
   umma_fence_after();
   kernel_release();
   const uint32_t tmem = tmem_at;
-  if (warp == 0 && lane == 0) {
+  if (warp == 0) {
     uint32_t it = 0;
     for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
       const uint32_t s = it % stages;
-      if (it >= (uint32_t)stages && !mbar_wait(&empty[s], ((it / stages) - 1) & 1u, &abort, w.limit)) {
+      if (it >= (uint32_t)stages && !warp_wait(&empty[s], ((it / stages) - 1) & 1u, &abort, w.limit)) {
         give_up(&abort, w);
         break;
       }
-      if (w.stall && it == 0) continue;
-      mbar_arrive_expect_tx(&full[s], kStage);
-      load_tile<1, 128, AT>(smem + s * kStage, &ma, c0, (int32_t)kb * kBK, su32(&full[s]));
-      load_tile<1, BN, BT>(smem + s * kStage + kA, &mb, r0, (int32_t)kb * kBK, su32(&full[s]));
+      if (!(w.stall && it == 0) && elect_one()) {
+        mbar_arrive_expect_tx(&full[s], kStage);
+        load_tile<1, 128, AT>(smem + s * kStage, &ma, c0, (int32_t)kb * kBK, su32(&full[s]));
+        load_tile<1, BN, BT>(smem + s * kStage + kA, &mb, r0, (int32_t)kb * kBK, su32(&full[s]));
+      }
+      __syncwarp();
     }
     // the stages still on their way, when something gave up: their copies end before the CTA does
     if (abort)
       for (uint32_t q = it > (uint32_t)stages ? it - stages : 0u; q < it; ++q)
         if (!(w.stall && q == 0)) mbar_wait_drain(&full[q % stages], (q / stages) & 1u);
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1) {
     uint32_t it = 0;
     for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
       const uint32_t s = it % stages;
-      if (!mbar_wait(&full[s], (it / stages) & 1u, &abort, w.limit)) {
+      if (!warp_wait(&full[s], (it / stages) & 1u, &abort, w.limit)) {
         give_up(&abort, w);
         break;
       }
       umma_fence_after();
       const uint64_t da = umma_desc<AT>(smem + s * kStage), db = umma_desc<BT>(smem + s * kStage + kA);
+      if (elect_one()) {
 #pragma unroll
-      for (int k = 0; k < kBK / 16; ++k)
-        umma<1>(tmem, da + k * (umma_k_step<AT>() >> 4), db + k * (umma_k_step<BT>() >> 4), umma_idesc<128, BN, AT, BT>(),
-                it > 0 || k > 0);
-      umma_commit<1>(&empty[s]);
+        for (int k = 0; k < kBK / 16; ++k)
+          umma<1>(tmem, da + k * (umma_k_step<AT>() >> 4), db + k * (umma_k_step<BT>() >> 4), umma_idesc<128, BN, AT, BT>(),
+                  it > 0 || k > 0);
+        umma_commit<1>(&empty[s]);
+      }
+      __syncwarp();
     }
-    umma_commit<1>(&done);
+    if (elect_one()) umma_commit<1>(&done);
     mbar_wait_drain(&done, 0);
   }
   __syncwarp();
@@ -404,7 +408,7 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
   __shared__ uint32_t tmem_at;
   __shared__ volatile int abort;
   const uint32_t smem = (su32(raw) + 1023u) & ~1023u;
-  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
   const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -436,7 +440,7 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
     c0 = (int32_t)((in / high) * kBN);
   };
   const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
-  if (warp == 0 && lane == 0) {
+  if (warp == 0) {
     uint32_t it = 0;
     bool ok = true;
     for (uint32_t t = first; t < n_tiles && ok; t += step) {
@@ -444,17 +448,19 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
       place(t, r0, c0);
       for (uint32_t kb = 0; kb < kb_all; ++kb, ++it) {
         const uint32_t s = it % kStages;
-        if (it >= kStages && !mbar_wait(&empty[s], ((it / kStages) - 1) & 1u, &abort, w.limit)) {
+        if (it >= kStages && !warp_wait(&empty[s], ((it / kStages) - 1) & 1u, &abort, w.limit)) {
           give_up(&abort, w);
           ok = false;
           break;
         }
-        if (w.stall && it == 0) continue;
-        uint32_t bar = su32(&full[s]);
-        if (rank == 0) mbar_arrive_expect_tx(&full[s], CG * kStage);
-        if (CG == 2) bar = cluster_map(bar, 0);
-        load_tile<CG, 128, AT>(smem + s * kStage, &ma, r0 + (int32_t)rank * 128, (int32_t)kb * kBK, bar);
-        load_tile<CG, kBNs, BT>(smem + s * kStage + kA, &mb, c0 + (int32_t)rank * kBNs, (int32_t)kb * kBK, bar);
+        if (!(w.stall && it == 0) && elect_one()) {
+          uint32_t bar = su32(&full[s]);
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], CG * kStage);
+          if (CG == 2) bar = cluster_map(bar, 0);
+          load_tile<CG, 128, AT>(smem + s * kStage, &ma, r0 + (int32_t)rank * 128, (int32_t)kb * kBK, bar);
+          load_tile<CG, kBNs, BT>(smem + s * kStage + kA, &mb, c0 + (int32_t)rank * kBNs, (int32_t)kb * kBK, bar);
+        }
+        __syncwarp();
       }
     }
     // after a wait that gave up: the copies still on their way end before the CTAs do.  Those of the second CTA
@@ -465,35 +471,38 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
     if (abort && rank == 0)
       for (uint32_t q = it > kStages ? it - kStages : 0u; q < it; ++q)
         if (!(w.stall && q == 0)) mbar_wait_drain(&full[q % kStages], (q / kStages) & 1u);
-  } else if (warp == 1 && lane == 0 && rank == 0) {
+  } else if (warp == 1 && rank == 0) {
     uint32_t it = 0, n = 0;
     bool ok = true;
     for (uint32_t t = first; t < n_tiles && ok; t += step, ++n) {
       const uint32_t half = n & 1u;
-      if (n >= 2 && !mbar_wait_cluster(&acc_empty[half], ((n >> 1) - 1) & 1u, &abort, w.limit)) {
+      if (n >= 2 && !warp_wait_cluster(&acc_empty[half], ((n >> 1) - 1) & 1u, &abort, w.limit)) {
         give_up(&abort, w);
         break;
       }
       umma_fence_after();
       for (uint32_t kb = 0; kb < kb_all; ++kb, ++it) {
         const uint32_t s = it % kStages;
-        if (!mbar_wait(&full[s], (it / kStages) & 1u, &abort, w.limit)) {
+        if (!warp_wait(&full[s], (it / kStages) & 1u, &abort, w.limit)) {
           give_up(&abort, w);
           ok = false;
           break;
         }
         umma_fence_after();
         const uint64_t da = umma_desc<AT>(smem + s * kStage), db = umma_desc<BT>(smem + s * kStage + kA);
+        if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < kBK / 16; ++k)
-          umma<CG>(tmem + half * kBN, da + k * (umma_k_step<AT>() >> 4), db + k * (umma_k_step<BT>() >> 4),
-                   umma_idesc<128 * CG, kBN, AT, BT>(), kb > 0 || k > 0);
-        umma_commit<CG>(&empty[s]);
+          for (int k = 0; k < kBK / 16; ++k)
+            umma<CG>(tmem + half * kBN, da + k * (umma_k_step<AT>() >> 4), db + k * (umma_k_step<BT>() >> 4),
+                     umma_idesc<128 * CG, kBN, AT, BT>(), kb > 0 || k > 0);
+          umma_commit<CG>(&empty[s]);
+        }
+        __syncwarp();
       }
-      if (ok) umma_commit<CG>(&acc_full[half]);
+      if (ok && elect_one()) umma_commit<CG>(&acc_full[half]);
     }
     if (!ok) {  // products still running end before their memory goes
-      umma_commit<CG>(&acc_full[n & 1u]);
+      if (elect_one()) umma_commit<CG>(&acc_full[n & 1u]);
       mbar_wait_drain(&acc_full[n & 1u], (n >> 1) & 1u);
     }
   } else if (warp >= 2) {

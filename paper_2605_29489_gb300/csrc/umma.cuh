@@ -25,6 +25,16 @@ constexpr uint32_t umma_k_step() {
   return T ? 16u * 128u : 32u;
 }
 
+// One thread of a warp whose threads are together, the same one every time.  The warps that issue copies and products go
+// through their loops whole and elect a thread for each step: operands then stay in uniform registers, where a
+// loop of one thread moved every one of them there again (a product of 256 x 256 x 16 was issued in about 150
+// cycles, and takes the tensor cores 128).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(one));
+  return one != 0;
+}
+
 // instruction descriptor: bf16 operands (T: mn-major), fp32 accumulators, an M x N product
 template <int M, int N, bool TA, bool TB>
 constexpr uint32_t umma_idesc() {
