@@ -576,14 +576,14 @@ mp_status mp_trace_read(mp_trace_range* out, uint64_t n);
  * mp_last_error() then names the injected fault.  Returns MP_ERR_INVALID_ARG for an unknown
  * kind.
  *
- * mp_debug_stall_pipeline(rounds): the index, merge and (bf16) linear kernels launched from now on never arm
+ * mp_debug_stall_pipeline(rounds): the index and merge kernels, and those of layer operators that fill rings (bf16 linear layers, the norms' backward pass), launched from now on never arm
  * the first slot of each CTA's shared-memory ring (its bulk copy is not issued), so the
  * consumers' wait for it cannot complete, and every pipeline wait (producer or consumer
  * mbarrier) gives up after `rounds` polling rounds instead of the default 2^21; in mp_plan calls of
  * more than 2^17 units one CTA of the planner's grid never comes to its barrier, where the
  * others give up after `rounds` polls.  The wait
  * that runs out sets the handle's error word; the accessors of that handle and of the
- * handles built from it (for linear layers mp_layer_status) return MP_ERR_TIMEOUT.  The waits that drain a CTA's own bulk
+ * handles built from it (for layer operators mp_layer_status) return MP_ERR_TIMEOUT.  The waits that drain a CTA's own bulk
  * copies before it exits keep the full limit, so no copy is in flight when a kernel
  * returns.  rounds = 0 turns the stall off.
  */

@@ -1581,7 +1581,7 @@ mp_status mp_layer_status(mp_stream stream) {
   if (e != cudaSuccess) return cuda_fail(e, "stream");
   uint32_t* w = layer_error_word();
   const uint32_t err = w ? __atomic_exchange_n(w, 0u, __ATOMIC_ACQ_REL) : 0u;
-  if (err & kErrTimeout) return fail(MP_ERR_TIMEOUT, "a bounded device wait in a linear layer gave up");
+  if (err & kErrTimeout) return fail(MP_ERR_TIMEOUT, "a bounded device wait in a layer operator gave up");
   if (err) return fail(MP_ERR_CUDA, "an internal check of the layer kernels failed");
   return MP_OK;
 }

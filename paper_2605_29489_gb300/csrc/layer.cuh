@@ -18,6 +18,17 @@ bool device_pointer(const void* p);
 uint32_t* layer_error_word();
 uint32_t stall_rounds();  // mp_debug_stall_pipeline
 
+// the bounded waits of a call's kernels
+struct Wait {
+  uint32_t* err;   // the host's error word
+  uint32_t limit;  // rounds of a wait
+  uint32_t stall;  // test hook: the first stage of each CTA is never filled
+};
+__device__ __forceinline__ void give_up(volatile int* abort, const Wait& w) {
+  *abort = 1;
+  atomicOr_system(w.err, kErrTimeout);
+}
+
 // scratch of one call: given back, in stream order, when the object goes
 struct Scratch {
   void* p = nullptr;
@@ -139,6 +150,7 @@ struct NormLaunch {
   const void *dy, *add;
   uint64_t lddy, ldadd, lddx;
   void *dx, *dweight, *dbias;  // each may be null
+  Wait wait;
 };
 cudaError_t launch_norm(const NormLaunch& p, cudaStream_t st);
 // bytes of scratch that the backward pass needs (0: none)
@@ -186,12 +198,13 @@ struct GemmLaunch {
   bool a_t, b_t;
   uint64_t inner;
   Epilogue e;
-  uint32_t* err;
-  uint32_t wait_limit, stall;
+  Wait wait;
 };
 // whether an operand can be read as it is (bf16: 16-byte rows); else it goes through pack()
 bool gemm_operand_ok(mp_dtype dtype, const Mat& m);
 mp_status launch_gemm(const GemmLaunch& g, cudaStream_t st);
+// dx (b along k) and dw (both operands along k) of a backward pass, in one launch where both are large
+mp_status launch_gemms(const GemmLaunch& dx, const GemmLaunch& dw, cudaStream_t st);
 // up to two copies of rows x cols elements (zeros without a source) in one launch
 struct Copy {
   Mat src;

@@ -144,14 +144,15 @@ mp_status linear_shape(mp_dtype dtype, mp_act act, uint64_t rows, uint64_t in, u
   return MP_OK;
 }
 
-mp_status error_word(GemmLaunch& g) {
-  g.err = layer_error_word();
-  if (!g.err) {
+mp_status make_wait(Wait& w) {
+  w.err = layer_error_word();
+  if (!w.err) {
     set_static_error("pinned host allocation failed");
     return MP_ERR_OOM;
   }
-  g.wait_limit = stall_rounds();
-  g.stall = g.wait_limit ? 1u : 0u;
+  const uint32_t stall = stall_rounds();
+  w.limit = stall ? stall : kWaitLimit;
+  w.stall = stall ? 1u : 0u;
   return MP_OK;
 }
 
@@ -238,6 +239,7 @@ mp_status norm_backward(const mp_norm_backward_args& a, mp_stream stream) {
   p.lddx = a.dx.ld;
   p.dweight = a.dweight;
   p.dbias = a.dbias;
+  if ((st = make_wait(p.wait)) != MP_OK) return st;
   Scratch s;
   if (const size_t bytes = norm_backward_scratch(p))
     if ((e = s.get(bytes, cs)) != cudaSuccess) return cuda_fail(e, "scratch");
@@ -266,7 +268,7 @@ mp_status linear(const mp_linear_args& a, mp_stream stream) {
   cudaStream_t cs = stream_of(stream);
   TraceScope tr(MP_TRACE_LINEAR, cs);
   GemmLaunch g = {};
-  if ((st = error_word(g)) != MP_OK) return st;
+  if ((st = make_wait(g.wait)) != MP_OK) return st;
   g.dtype = a.dtype;
   g.a = Mat{a.x.data, a.x.ld};
   g.b = Mat{a.w.data, a.w.ld};
@@ -325,7 +327,7 @@ mp_status linear_backward(const mp_linear_backward_args& a, mp_stream stream) {
     return MP_OK;
   }
   GemmLaunch g = {};
-  if ((st = error_word(g)) != MP_OK) return st;
+  if ((st = make_wait(g.wait)) != MP_OK) return st;
   g.dtype = a.dtype;
   // the scratch: dz, its column sums, operands that have to be copied
   const bool products = a.dx.data || a.dw.data;
@@ -363,21 +365,22 @@ mp_status linear_backward(const mp_linear_backward_args& a, mp_stream stream) {
     return cuda_fail(e, "linear kernel");
   if ((e = re.copy(a.dtype, s, cs)) != cudaSuccess) return cuda_fail(e, "copy kernel");
   g.a = dz;
+  GemmLaunch g2 = g;
   if (a.dx.data) {
     g.b = w;
     g.b_t = true;
     g.inner = a.out;
     g.e = Epilogue{a.rows, a.in, nullptr, MP_ACT_NONE, Mat{}, Mat{a.dx_add.data, a.dx_add.ld}, a.dx.data, nullptr, a.dx.ld, 0};
-    if ((st = launch_gemm(g, cs)) != MP_OK) return st;
   }
   if (a.dw.data) {
-    g.b = x;
-    g.a_t = g.b_t = true;
-    g.inner = a.rows;
-    g.e = Epilogue{a.out, a.in, nullptr, MP_ACT_NONE, Mat{}, Mat{a.dw_add.data, a.dw_add.ld}, a.dw.data, nullptr, a.dw.ld, 0};
-    if ((st = launch_gemm(g, cs)) != MP_OK) return st;
+    g2.b = x;
+    g2.a_t = g2.b_t = true;
+    g2.inner = a.rows;
+    g2.e = Epilogue{a.out, a.in, nullptr, MP_ACT_NONE, Mat{}, Mat{a.dw_add.data, a.dw_add.ld}, a.dw.data, nullptr, a.dw.ld, 0};
   }
-  return MP_OK;
+  if (a.dx.data && a.dw.data) return launch_gemms(g, g2, cs);
+  if (a.dx.data) return launch_gemm(g, cs);
+  return a.dw.data ? launch_gemm(g2, cs) : MP_OK;
 }
 
 template <typename A>

@@ -21,6 +21,7 @@
 #include <dlfcn.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "layer.cuh"
 #include "umma.cuh"
@@ -31,47 +32,66 @@ namespace {
 
 // ---- the epilogue -------------------------------------------------------------------------------
 
-// act(z).  FAST: bf16 results, where the fast exponential's 2 ulp do not show.
+// The activations as z times a gate p(z), and their derivatives p + z p'.  SiLU: p = sigmoid(z); GELU: p = Phi(z), the
+// normal distribution function; its tanh form: p = (1 + tanh(u)) / 2 = sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3),
+// which keeps its relative accuracy where 1 + tanh cancels.  FAST: bf16 results, where the fast exponential's 2 ulp
+// do not show, nor the 1.5e-7 by which Abramowitz and Stegun's 7.1.26 is off erf; its exponential is the one that
+// the derivative needs.  (4096 x 14336, the backward pass's elementwise part: GELU 130 us with erff, tanh 119 with tanhf, SiLU 82.)
+template <bool FAST>
+__device__ __forceinline__ float exp_of(float z) {
+  return FAST ? __expf(z) : expf(z);
+}
+template <bool FAST>
+__device__ __forceinline__ float inverse(float z) {
+  return FAST ? __fdividef(1.0f, z) : 1.0f / z;
+}
 template <bool FAST>
 __device__ __forceinline__ float sigmoid(float z) {
-  return FAST ? __fdividef(1.0f, 1.0f + __expf(-z)) : 1.0f / (1.0f + expf(-z));
+  return inverse<FAST>(1.0f + exp_of<FAST>(-z));
 }
-constexpr float kRootHalf = 0.70710678118654752f, kRoot2Pi = 0.79788456080286536f, kInvRoot2Pi = 0.39894228040143268f;
+constexpr float kRootHalf = 0.70710678118654752f, kRoot8Pi = 1.59576912160573071f, kInvRoot2Pi = 0.39894228040143268f;
 constexpr float kTanhCubic = 0.044715f;
 
-template <int ACT, bool FAST>
-__device__ __forceinline__ float act_of(float z) {
-  if constexpr (ACT == MP_ACT_RELU) return z > 0.0f ? z : (z == z ? 0.0f : z);
-  if constexpr (ACT == MP_ACT_SILU) return z * sigmoid<FAST>(z);
-  if constexpr (ACT == MP_ACT_GELU) return 0.5f * z * (1.0f + erff(z * kRootHalf));
-  if constexpr (ACT == MP_ACT_GELU_TANH) return 0.5f * z * (1.0f + tanhf(kRoot2Pi * fmaf(kTanhCubic * z * z, z, z)));
-  return z;
-}
-// act(z) in a and act'(z) in g: they share what costs most
-template <int ACT, bool FAST>
+// act(z) in a and, where G is set, act'(z) in g
+template <int ACT, bool FAST, bool G>
 __device__ __forceinline__ void act_both(float z, float& a, float& g) {
   a = z;
   g = 1.0f;
   if constexpr (ACT == MP_ACT_RELU) {
-    a = act_of<ACT, FAST>(z);
+    a = z > 0.0f ? z : (z == z ? 0.0f : z);
     g = z > 0.0f ? 1.0f : 0.0f;
   }
   if constexpr (ACT == MP_ACT_SILU) {
-    const float s = sigmoid<FAST>(z);
-    a = z * s;
-    g = s * fmaf(z, 1.0f - s, 1.0f);
+    const float p = sigmoid<FAST>(z);
+    a = z * p;
+    g = p * fmaf(z, 1.0f - p, 1.0f);
   }
   if constexpr (ACT == MP_ACT_GELU) {
-    const float s = 0.5f * (1.0f + erff(z * kRootHalf));
-    a = z * s;
-    g = fmaf(z, kInvRoot2Pi * expf(-0.5f * z * z), s);
+    const float e = FAST || G ? exp_of<FAST>(-0.5f * z * z) : 0.0f;
+    float p;
+    if constexpr (FAST) {
+      const float t = inverse<FAST>(fmaf(0.3275911f * kRootHalf, fabsf(z), 1.0f));
+      const float q = 0.5f * e * t *
+                      fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+      p = z < 0.0f ? q : 1.0f - q;
+    } else {
+      p = 0.5f * (1.0f + erff(z * kRootHalf));
+    }
+    a = z * p;
+    g = fmaf(z, kInvRoot2Pi * e, p);
   }
   if constexpr (ACT == MP_ACT_GELU_TANH) {
-    const float t = tanhf(kRoot2Pi * fmaf(kTanhCubic * z * z, z, z)), s = 0.5f * (1.0f + t);
-    const float c = fminf(fmaxf(z, -16.0f), 16.0f);  // t is +-1 from there on: no 0 * infinity
-    a = z * s;
-    g = fmaf(0.5f * c * (1.0f - t * t), kRoot2Pi * fmaf(3.0f * kTanhCubic * c, c, 1.0f), s);
+    const float p = sigmoid<FAST>(kRoot8Pi * fmaf(kTanhCubic * z * z, z, z));
+    const float c = fminf(fmaxf(z, -16.0f), 16.0f);  // p is 0 or 1 from there on: no 0 * infinity
+    a = z * p;
+    g = fmaf(c * p * (1.0f - p), kRoot8Pi * fmaf(3.0f * kTanhCubic * c, c, 1.0f), p);
   }
+}
+template <int ACT, bool FAST>
+__device__ __forceinline__ float act_of(float z) {
+  float a, g;
+  act_both<ACT, FAST, false>(z, a, g);
+  return a;
 }
 
 template <bool FAST, int N>
@@ -213,12 +233,6 @@ constexpr int kGemmThreads = 32 * kWarps;       // a TMA warp, a warp that issue
 
 using bf16 = __nv_bfloat16;
 
-struct Wait {
-  uint32_t* err;   // the host's error word
-  uint32_t limit;  // rounds of a wait
-  uint32_t stall;  // test hook: the first stage is never filled
-};
-
 // loads ROWS rows (m or n, from r0 on) x 64 k (from k0 on) of an operand
 template <int CG, int ROWS, bool T>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int32_t r0, int32_t k0, uint32_t bar) {
@@ -228,11 +242,6 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
   } else {
     tma_load_2d<CG>(dst, map, k0, r0, bar);
   }
-}
-
-__device__ __forceinline__ void give_up(volatile int* abort, const Wait& w) {
-  *abort = 1;
-  atomicOr_system(w.err, kErrTimeout);
 }
 
 // a warp's bounded wait on an mbarrier that threads of another CTA arrive on
@@ -392,16 +401,26 @@ __global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_consta
   if (warp == 1) tmem_free<1>(tmem, kCols);
 }
 
-// Many rows: tiles of CG * 128 rows x 256 columns, the next tile's products during this one's epilogue.  a: the rows'
-// operand, b: the columns'.
-template <int CG, bool AT, bool BT>
+// A product of gemm_kernel: its maps are arguments of their own.
+struct Product {
+  Epi<bf16> e;
+  uint32_t kb, tiles_r, tiles_c;  // stages of the inner dimension; tiles of 256 rows and of 256 columns
+};
+
+// Many rows: tiles of 256 x 256 by pairs of CTAs (128 rows each, half of the columns' operand each), persistent, the next
+// tile's products during this one's epilogue.  a: the rows' operand, b: the columns'.  With TWO, a second product
+// (both operands stored along k) follows in the same launch: the tiles of a backward pass's dx are few and long (256
+// tiles of 224 stages on 76 pairs are 3.4 rounds, which took the time of 4), and those of dw fill up what they leave.
+// Bound by the tensor cores: 4096 rows, 4096 -> 14336, 273 us alone (1764 TFLOP/s, cuBLAS 266 in the same call).
+template <bool AT, bool BT, bool TWO>
 __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constant__ CUtensorMap ma,
-                                                            const __grid_constant__ CUtensorMap mb, const Epi<bf16> e,
-                                                            uint32_t kb_all, uint32_t tiles_r, uint32_t tiles_c,
+                                                            const __grid_constant__ CUtensorMap mb, const Product p1,
+                                                            const __grid_constant__ CUtensorMap ma2,
+                                                            const __grid_constant__ CUtensorMap mb2, const Product p2,
                                                             const Wait w) {
-  constexpr int kBN = 256, kBNs = kBN / CG;  // columns of a tile, and those whose operand this CTA holds
-  constexpr uint32_t kA = 128 * 128, kB = kBNs * 128, kStage = kA + kB;
-  constexpr int kStages = CG == 2 ? 6 : 4;
+  constexpr int kTile = 256;
+  constexpr uint32_t kHalf = 128 * 128, kStage = 2 * kHalf;  // either operand's part of a stage
+  constexpr int kStages = 6;
   constexpr uint32_t kGroup = 8;  // row tiles that go down the columns together: what they read stays in L2
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
@@ -409,7 +428,7 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
   __shared__ volatile int abort;
   const uint32_t smem = (su32(raw) + 1023u) & ~1023u;
   const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
-  const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+  const uint32_t rank = cluster_rank();
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&full[s], 1);
@@ -417,52 +436,71 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&acc_full[s], 1);
-      mbar_init(&acc_empty[s], CG * 4);
+      mbar_init(&acc_empty[s], 2 * 4);
     }
     mbar_fence_init();
     abort = 0;
     prefetch_map(&ma);
     prefetch_map(&mb);
+    if (TWO) {
+      prefetch_map(&ma2);
+      prefetch_map(&mb2);
+    }
   }
   kernel_wait();
-  if (warp == 1) tmem_alloc<CG>(&tmem_at, 512);
+  if (warp == 1) tmem_alloc<2>(&tmem_at, 512);
   umma_fence_before();
   __syncthreads();
-  if (CG == 2) cluster_sync();  // the other CTA's barriers are there
+  cluster_sync();  // the other CTA's barriers are there
   umma_fence_after();
   kernel_release();
   const uint32_t tmem = tmem_at;
-  const uint32_t n_tiles = tiles_r * tiles_c;
-  auto place = [&](uint32_t t, int32_t& r0, int32_t& c0) {
-    const uint32_t per = kGroup * tiles_c, g = t / per, in = t % per;
-    const uint32_t high = min(kGroup, tiles_r - g * kGroup);
-    r0 = (int32_t)((g * kGroup + in % high) * (128u * CG));
-    c0 = (int32_t)((in / high) * kBN);
+  const uint32_t pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  auto place = [&](const Product& p, uint32_t t, int32_t& r0, int32_t& c0) {
+    const uint32_t per = kGroup * p.tiles_c, g = t / per, in = t % per;
+    const uint32_t high = min(kGroup, p.tiles_r - g * kGroup);
+    r0 = (int32_t)((g * kGroup + in % high) * kTile);
+    c0 = (int32_t)((in / high) * kTile);
   };
-  const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
+  // This pair's tiles: every pairs-th of the first product.  Of the second, the pairs that had one fewer of the first
+  // begin with as many as make up for it (`lead` each), then every pairs-th, those pairs first.  f(second, product,
+  // tile) returns whether to go on.
+  const uint32_t n1 = p1.tiles_r * p1.tiles_c, n2 = TWO ? p2.tiles_r * p2.tiles_c : 0u;
+  auto for_tiles = [&](auto f) {
+    for (uint32_t t = pair; t < n1; t += pairs)
+      if (!f(std::false_type(), p1, t)) return;
+    if constexpr (TWO) {
+      const uint32_t longer = n1 % pairs, others = pairs - longer;
+      const uint32_t lead = longer ? min(p1.kb / p2.kb, n2 / others) : 0u;
+      if (pair >= longer)
+        for (uint32_t j = 0; j < lead; ++j)
+          if (!f(std::true_type(), p2, pair - longer + j * others)) return;
+      for (uint32_t t = lead * others + (pair >= longer ? pair - longer : pair + others); t < n2; t += pairs)
+        if (!f(std::true_type(), p2, t)) return;
+    }
+  };
   if (warp == 0) {
     uint32_t it = 0;
-    bool ok = true;
-    for (uint32_t t = first; t < n_tiles && ok; t += step) {
+    for_tiles([&](auto second, const Product& p, uint32_t t) {
+      constexpr bool S = decltype(second)::value, A = AT || S, B = BT || S;
       int32_t r0, c0;
-      place(t, r0, c0);
-      for (uint32_t kb = 0; kb < kb_all; ++kb, ++it) {
+      place(p, t, r0, c0);
+      for (uint32_t kb = 0; kb < p.kb; ++kb, ++it) {
         const uint32_t s = it % kStages;
         if (it >= kStages && !warp_wait(&empty[s], ((it / kStages) - 1) & 1u, &abort, w.limit)) {
           give_up(&abort, w);
-          ok = false;
-          break;
+          return false;
         }
         if (!(w.stall && it == 0) && elect_one()) {
-          uint32_t bar = su32(&full[s]);
-          if (rank == 0) mbar_arrive_expect_tx(&full[s], CG * kStage);
-          if (CG == 2) bar = cluster_map(bar, 0);
-          load_tile<CG, 128, AT>(smem + s * kStage, &ma, r0 + (int32_t)rank * 128, (int32_t)kb * kBK, bar);
-          load_tile<CG, kBNs, BT>(smem + s * kStage + kA, &mb, c0 + (int32_t)rank * kBNs, (int32_t)kb * kBK, bar);
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * kStage);
+          const uint32_t bar = cluster_map(su32(&full[s]), 0);
+          load_tile<2, 128, A>(smem + s * kStage, S ? &ma2 : &ma, r0 + (int32_t)rank * 128, (int32_t)kb * kBK, bar);
+          load_tile<2, 128, B>(smem + s * kStage + kHalf, S ? &mb2 : &mb, c0 + (int32_t)rank * 128, (int32_t)kb * kBK, bar);
         }
         __syncwarp();
       }
-    }
+      return true;
+    });
     // after a wait that gave up: the copies still on their way end before the CTAs do.  Those of the second CTA
     // count on the first one's barriers, which only that one can wait for: it stays a millisecond, a
     // thousand times what a copy takes
@@ -474,71 +512,67 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
   } else if (warp == 1 && rank == 0) {
     uint32_t it = 0, n = 0;
     bool ok = true;
-    for (uint32_t t = first; t < n_tiles && ok; t += step, ++n) {
+    for_tiles([&](auto second, const Product& p, uint32_t) {
+      constexpr bool S = decltype(second)::value, A = AT || S, B = BT || S;
       const uint32_t half = n & 1u;
-      if (n >= 2 && !warp_wait_cluster(&acc_empty[half], ((n >> 1) - 1) & 1u, &abort, w.limit)) {
-        give_up(&abort, w);
-        break;
-      }
+      ok = n < 2 || warp_wait_cluster(&acc_empty[half], ((n >> 1) - 1) & 1u, &abort, w.limit);
       umma_fence_after();
-      for (uint32_t kb = 0; kb < kb_all; ++kb, ++it) {
+      for (uint32_t kb = 0; ok && kb < p.kb; ++kb, ++it) {
         const uint32_t s = it % kStages;
-        if (!warp_wait(&full[s], (it / kStages) & 1u, &abort, w.limit)) {
-          give_up(&abort, w);
-          ok = false;
-          break;
-        }
+        ok = warp_wait(&full[s], (it / kStages) & 1u, &abort, w.limit);
+        if (!ok) break;
         umma_fence_after();
-        const uint64_t da = umma_desc<AT>(smem + s * kStage), db = umma_desc<BT>(smem + s * kStage + kA);
+        const uint64_t da = umma_desc<A>(smem + s * kStage), db = umma_desc<B>(smem + s * kStage + kHalf);
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < kBK / 16; ++k)
-            umma<CG>(tmem + half * kBN, da + k * (umma_k_step<AT>() >> 4), db + k * (umma_k_step<BT>() >> 4),
-                     umma_idesc<128 * CG, kBN, AT, BT>(), kb > 0 || k > 0);
-          umma_commit<CG>(&empty[s]);
+            umma<2>(tmem + half * kTile, da + k * (umma_k_step<A>() >> 4), db + k * (umma_k_step<B>() >> 4),
+                    umma_idesc<256, kTile, A, B>(), kb > 0 || k > 0);
+          umma_commit<2>(&empty[s]);
         }
         __syncwarp();
       }
-      if (ok && elect_one()) umma_commit<CG>(&acc_full[half]);
-    }
+      if (!ok) return false;
+      if (elect_one()) umma_commit<2>(&acc_full[half]);
+      ++n;
+      return true;
+    });
     if (!ok) {  // products still running end before their memory goes
-      if (elect_one()) umma_commit<CG>(&acc_full[n & 1u]);
+      give_up(&abort, w);
+      if (elect_one()) umma_commit<2>(&acc_full[n & 1u]);
       mbar_wait_drain(&acc_full[n & 1u], (n >> 1) & 1u);
     }
   } else if (warp >= 2) {
     const uint32_t quad = warp & 3u, row = quad * 32u + lane;
     uint32_t n = 0;
-    for (uint32_t t = first; t < n_tiles; t += step, ++n) {
+    for_tiles([&](auto, const Product& p, uint32_t t) {
       const uint32_t half = n & 1u;
       int32_t r0, c0;
-      place(t, r0, c0);
+      place(p, t, r0, c0);
       if (!warp_wait(&acc_full[half], (n >> 1) & 1u, &abort, w.limit) || abort) {
         if (lane == 0) give_up(&abort, w);
-        break;
+        return false;
       }
       umma_fence_after();
 #pragma unroll 1
-      for (int j0 = 0; j0 < kBN; j0 += 16) {
+      for (int j0 = 0; j0 < kTile; j0 += 16) {
         float v[16];
-        tmem_load16(tmem + ((quad * 32u) << 16) + half * kBN + j0, v);
-        epi_run<bf16, 16>(e, (uint32_t)r0 + rank * 128u + row, (uint32_t)(c0 + j0), v);
+        tmem_load16(tmem + ((quad * 32u) << 16) + half * kTile + j0, v);
+        epi_run<bf16, 16>(p.e, (uint32_t)r0 + rank * 128u + row, (uint32_t)(c0 + j0), v);
       }
       umma_fence_before();
       __syncwarp();
-      if (lane == 0) {
-        if (CG == 2)
-          cluster_arrive(cluster_map(su32(&acc_empty[half]), 0));
-        else
-          mbar_arrive(&acc_empty[half]);
-      }
-    }
+      if (lane == 0) cluster_arrive(cluster_map(su32(&acc_empty[half]), 0));
+      ++n;
+      return true;
+    });
   }
   __syncwarp();
   umma_fence_before();
   __syncthreads();
-  if (CG == 2) cluster_sync();
+  cluster_sync();
   umma_fence_after();
-  if (warp == 1) tmem_free<CG>(tmem, 512);
+  if (warp == 1) tmem_free<2>(tmem, 512);
 }
 
 // ---- fp32 products --------------------------------------------------------------------------------
@@ -651,26 +685,33 @@ __global__ void __launch_bounds__(256, R == 1 ? 2 : 1) gemm_f32_kernel(const flo
 template <typename T>
 struct DzArgs {
   uint64_t rows, rows_each, lddy, ldpre, ldmul, lddz, lddmul;
-  uint32_t cols;
+  uint32_t cols, parts, wide;  // parts: runs of rows, each a CTA's
+  uint32_t cluster;            // the parts are a cluster, which adds up their column sums
   const T *dy, *pre, *mul;
-  T *dz, *dmul;
-  float* part;  // [gridDim.y][cols] column sums, or null
+  T *dz, *dmul, *db;
+  float* part;  // [parts][cols] column sums where the parts are no cluster
 };
 
-// 32 threads x V columns and a run of rows to a CTA, the rows dealt out to its eight warps; the warps' column sums are
-// added in order
+// A CTA has 32 V `wide` columns (wide: the warps side by side, 1 to 8) and a run of rows, 8 / wide rows at a time.  Four
+// CTAs to an SM hide what a row waits for better than more rows in flight with fewer: 4096 x 14336, SiLU, three
+// matrices read and one written, 82 us; two rows and three CTAs 94, two and two 114 (a copy of as many bytes takes 76).  The
+// column sums of warps, then of CTAs, are added in order.
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(256) dz_kernel(const DzArgs<T> p) {
+__global__ void __launch_bounds__(256, 4) dz_kernel(const DzArgs<T> p) {
   kernel_begin();
   constexpr bool FAST = sizeof(T) == 2;
-  __shared__ float sum[8][32 * V + 1];
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  const uint32_t c = (blockIdx.x * 32u + lane) * V;
-  const uint64_t q0 = blockIdx.y * p.rows_each, q1 = q0 + p.rows_each < p.rows ? q0 + p.rows_each : p.rows;
+  __shared__ float sum[8][32 * V + 1], total[8 * 32 * V];
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, deep = 8u / p.wide;
+  const uint32_t across = 32u * V * p.wide;
+  // a cluster's CTAs are neighbours; else those with the same rows are
+  const uint32_t blocks = (p.cols + across - 1) / across;
+  const uint32_t run = p.cluster ? blockIdx.x % p.parts : blockIdx.x / blocks;
+  const uint32_t c0 = (p.cluster ? blockIdx.x / p.parts : blockIdx.x % blocks) * across;
+  const uint32_t c = c0 + (warp % p.wide * 32u + lane) * V;
+  const uint64_t q0 = run * p.rows_each, q1 = q0 + p.rows_each < p.rows ? q0 + p.rows_each : p.rows;
   float s[V] = {};
   if (c < p.cols) {
-#pragma unroll 2
-    for (uint64_t r = q0 + warp; r < q1; r += 8) {
+    for (uint64_t r = q0 + warp / p.wide; r < q1; r += deep) {
       const Pack<T, V> dq = load_pack<T, V>(p.dy + r * p.lddy + c);
       Pack<T, V> zq, mq;
       if (p.pre) zq = load_pack<T, V>(p.pre + r * p.ldpre + c);
@@ -682,7 +723,7 @@ __global__ void __launch_bounds__(256) dz_kernel(const DzArgs<T> p) {
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         float a, g;
-        act_both<ACT, FAST>(z[k], a, g);
+        act_both<ACT, FAST, true>(z[k], a, g);
         om[k] = d[k] * a;
         if (ACT != MP_ACT_NONE) d[k] *= g;
         if (p.mul) d[k] *= m[k];
@@ -692,19 +733,25 @@ __global__ void __launch_bounds__(256) dz_kernel(const DzArgs<T> p) {
       if (p.dmul) store_pack<T, V>(p.dmul + r * p.lddmul + c, pack<T, V>(om));
     }
   }
-  if (!p.part) return;
+  if (!p.db) return;
 #pragma unroll
   for (int k = 0; k < V; ++k) sum[warp][lane * V + k] = s[k];
   __syncthreads();
-  for (uint32_t k = threadIdx.x; k < 32u * V; k += 256u) {
-    const uint32_t cc = blockIdx.x * 32u * V + k;
-    if (cc < p.cols) {
-      float v = 0.0f;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v += sum[q][k];
-      p.part[(uint64_t)blockIdx.y * p.cols + cc] = v;
-    }
+  for (uint32_t k = threadIdx.x; k < across; k += 256u) {
+    float v = 0.0f;
+    for (uint32_t q = 0; q < deep; ++q) v += sum[q * p.wide + k / (32u * V)][k % (32u * V)];
+    total[k] = v;
+    if (!p.cluster && c0 + k < p.cols) p.part[(uint64_t)run * p.cols + c0 + k] = v;
   }
+  if (!p.cluster) return;
+  cluster_sync();
+  for (uint32_t k = threadIdx.x; k < across; k += 256u)  // the columns are dealt out to the CTAs
+    if (k % p.parts == run && c0 + k < p.cols) {
+      float v = 0.0f;
+      for (uint32_t q = 0; q < p.parts; ++q) v += cluster_load1(cluster_map(su32(&total[k]), q));
+      p.db[c0 + k] = Elem<T>::store(v);
+    }
+  cluster_sync();
 }
 
 // copies (or zeros: no source) of up to two matrices, blockIdx.y saying which
@@ -848,54 +895,80 @@ cudaError_t launch_split_of(int bn, const CUtensorMap& ma, const CUtensorMap& mb
   return launch_split<128, AT, BT>(ma, mb, e, kb, split, stages, w, st);
 }
 
-template <int CG, bool AT, bool BT>
-cudaError_t launch_big(const CUtensorMap& ma, const CUtensorMap& mb, const Epi<bf16>& e, uint32_t kb,
-                       const Wait& w, cudaStream_t st) {
-  const uint32_t tiles_r = (e.rows + 128u * CG - 1) / (128u * CG), tiles_c = (e.cols + 255u) / 256u;
-  const uint64_t tiles = (uint64_t)tiles_r * tiles_c;
-  const unsigned groups = (unsigned)std::min<uint64_t>(tiles, (uint64_t)device_sms() / CG);
-  const size_t smem = CG == 2 ? 6 * 32768 + 1024 : 4 * 49152 + 1024;
-  return launch_cluster(gemm_kernel<CG, AT, BT>, groups * CG, kGemmThreads, CG, smem, st, ma, mb, e, kb, tiles_r, tiles_c, w);
+struct Prepared {  // a bf16 product on its way to a launch
+  CUtensorMap ma, mb;  // of the rows' operand and of the columns'
+  Product p;
+};
+
+bool large_product(const Epilogue& e) {
+  const uint64_t tiles = ((e.rows + 255) / 256) * ((e.cols + 255) / 256);
+  return e.rows > 128 && tiles * 2 >= (uint64_t)device_sms() / 2;
+}
+
+uint32_t inner_stages(const GemmLaunch& g) { return (uint32_t)((g.inner + kBK - 1) / kBK); }
+
+mp_status prepare_large(const GemmLaunch& g, Prepared& q) {
+  mp_status s;
+  if ((s = make_map(&q.ma, g.a, g.a_t, g.e.rows, g.inner, 128u)) != MP_OK) return s;
+  if ((s = make_map(&q.mb, g.b, g.b_t, g.e.cols, g.inner, 128u)) != MP_OK) return s;
+  q.p.e = epi_of<bf16>(g.e);
+  q.p.kb = inner_stages(g);
+  q.p.tiles_r = (uint32_t)((g.e.rows + 255) / 256);
+  q.p.tiles_c = (uint32_t)((g.e.cols + 255) / 256);
+  const uint64_t tiles = (uint64_t)q.p.tiles_r * q.p.tiles_c;
+  if (tiles > 0x7FFFFFFFull / 2) {
+    set_static_error("the output has too many tiles");
+    return MP_ERR_UNSUPPORTED;
+  }
+  return MP_OK;
+}
+
+template <bool AT, bool BT, bool TWO>
+mp_status launch_large(const GemmLaunch& g, const Prepared& a, const Prepared& b, cudaStream_t st) {
+  const uint64_t tiles = (uint64_t)a.p.tiles_r * a.p.tiles_c + (TWO ? (uint64_t)b.p.tiles_r * b.p.tiles_c : 0u);
+  const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)device_sms() / 2);
+  const cudaError_t r = launch_cluster(gemm_kernel<AT, BT, TWO>, pairs * 2, kGemmThreads, 2, 6 * 32768 + 1024, st, a.ma, a.mb,
+                                       a.p, b.ma, b.mb, b.p, g.wait);
+  return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
 
 mp_status gemm_bf16(const GemmLaunch& g, cudaStream_t st) {
-  const Epi<bf16> e = epi_of<bf16>(g.e);
-  const uint64_t kb64 = (g.inner + kBK - 1) / kBK;
-  const uint32_t kb = (uint32_t)kb64;
-  const uint64_t sms = (uint64_t)device_sms();
-  const uint64_t big_tiles = ((g.e.rows + 255) / 256) * ((g.e.cols + 255) / 256);
-  const bool big = g.e.rows > 128 && big_tiles * 2 >= sms / 2;
-  // split: rows of a tile, and the CTAs that share it
-  int bn = 128;
-  if (!g.a_t) bn = g.e.rows <= 16 ? 16 : g.e.rows <= 32 ? 32 : g.e.rows <= 64 ? 64 : 128;
-  CUtensorMap ma, mb;  // of the rows' operand and of the columns'
   mp_status s;
-  if ((s = make_map(&ma, g.a, g.a_t, g.e.rows, g.inner, big ? 128u : (uint32_t)bn)) != MP_OK) return s;
-  if ((s = make_map(&mb, g.b, g.b_t, g.e.cols, g.inner, 128u)) != MP_OK) return s;
-  const Wait w = {g.err, g.wait_limit ? g.wait_limit : kWaitLimit, g.stall};
-  cudaError_t r;
-  if (big) {
-    r = g.a_t ? launch_big<2, true, true>(ma, mb, e, kb, w, st)
-        : g.b_t ? launch_big<2, false, true>(ma, mb, e, kb, w, st)
-                : launch_big<2, false, false>(ma, mb, e, kb, w, st);
-  } else {
-    const uint64_t tiles = ((g.e.rows + bn - 1) / bn) * ((g.e.cols + 127) / 128);
-    // As many CTAs as share a tile while three to an SM hold them all and each has two stages at least, and as many
-    // stages as shared memory holds then (with a tenth of the SMs' places to spare: clusters do not fill every one).
-    // One row, 4096 -> 14336, 112 tiles: 26.8 us unsplit, 23.0 with two CTAs of 5 stages, 21.9 with four of 3, 29 with
-    // four of 4 stages, which do not all fit; 24 rows, 14336 -> 4096, 32 tiles: 83 us unsplit, 25.1 with eight of 5.
-    const int stage = 128 * 128 + bn * 128;
-    auto stages_with = [&](uint64_t ctas) {
-      const uint64_t per_sm = std::max<uint64_t>(1, std::min<uint64_t>(4, (ctas * 11 + sms * 10 - 1) / (sms * 10)));
-      return (int)std::min<uint64_t>(6, (228 * 1024 / per_sm - 2560) / stage);
-    };
-    unsigned split = 1;
-    while (split < 8 && tiles * split * 2 <= sms * 3 && kb >= 4 * split && stages_with(tiles * split * 2) >= 2) split *= 2;
-    const int stages = std::max(2, stages_with(tiles * split));
-    r = g.a_t ? launch_split_of<true, true>(bn, mb, ma, e, kb, split, stages, w, st)
-        : g.b_t ? launch_split_of<true, false>(bn, mb, ma, e, kb, split, stages, w, st)
-                : launch_split_of<false, false>(bn, mb, ma, e, kb, split, stages, w, st);
+  if (large_product(g.e)) {
+    Prepared q;
+    if ((s = prepare_large(g, q)) != MP_OK) return s;
+    return g.a_t   ? launch_large<true, true, false>(g, q, q, st)
+           : g.b_t ? launch_large<false, true, false>(g, q, q, st)
+                   : launch_large<false, false, false>(g, q, q, st);
   }
+  const Epi<bf16> e = epi_of<bf16>(g.e);
+  const uint32_t kb = inner_stages(g);
+  const uint64_t sms = (uint64_t)device_sms();
+  int bn = 128;  // rows of a tile
+  if (!g.a_t) bn = g.e.rows <= 16 ? 16 : g.e.rows <= 32 ? 32 : g.e.rows <= 64 ? 64 : 128;
+  CUtensorMap ma, mb;
+  if ((s = make_map(&ma, g.a, g.a_t, g.e.rows, g.inner, (uint32_t)bn)) != MP_OK) return s;
+  if ((s = make_map(&mb, g.b, g.b_t, g.e.cols, g.inner, 128u)) != MP_OK) return s;
+  const uint64_t tiles = ((g.e.rows + bn - 1) / bn) * ((g.e.cols + 127) / 128);
+  if (tiles > 0x7FFFFFFFull / 8) {
+    set_static_error("the output has too many tiles");
+    return MP_ERR_UNSUPPORTED;
+  }
+  // As many CTAs as share a tile while three to an SM hold them all and each has two stages at least, and as many
+  // stages as shared memory holds then (with a tenth of the SMs' places to spare: clusters do not fill every one).
+  // One row, 4096 -> 14336, 112 tiles: 26.8 us unsplit, 23.0 with two CTAs of 5 stages, 21.9 with four of 3, 29 with
+  // four of 4 stages, which do not all fit; 24 rows, 14336 -> 4096, 32 tiles: 83 us unsplit, 25.1 with eight of 5.
+  const int stage = 128 * 128 + bn * 128;
+  auto stages_with = [&](uint64_t ctas) {
+    const uint64_t per_sm = std::max<uint64_t>(1, std::min<uint64_t>(4, (ctas * 11 + sms * 10 - 1) / (sms * 10)));
+    return (int)std::min<uint64_t>(6, (228 * 1024 / per_sm - 2560) / stage);
+  };
+  unsigned split = 1;
+  while (split < 8 && tiles * split * 2 <= sms * 3 && kb >= 4 * split && stages_with(tiles * split * 2) >= 2) split *= 2;
+  const int stages = std::max(2, stages_with(tiles * split));
+  const cudaError_t r = g.a_t   ? launch_split_of<true, true>(bn, mb, ma, e, kb, split, stages, g.wait, st)
+                        : g.b_t ? launch_split_of<true, false>(bn, mb, ma, e, kb, split, stages, g.wait, st)
+                                : launch_split_of<false, false>(bn, mb, ma, e, kb, split, stages, g.wait, st);
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
 
@@ -920,17 +993,27 @@ mp_status gemm_f32(const GemmLaunch& g, cudaStream_t st) {
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
 
-template <typename T, int V, int ACT>
-cudaError_t dz_launch(const DzArgs<T>& a, dim3 grid, cudaStream_t st) {
-  return launch_kernel(true, dz_kernel<T, V, ACT>, grid, 256, 0, st, a);
-}
-
-constexpr uint32_t kDzParts = 64;  // runs of rows at most: their column sums are read again
-
-uint32_t dz_parts(const DzLaunch& p, int v) {
-  const uint64_t across = (p.cols + 32u * v - 1) / (32u * v);
-  const uint64_t want = std::max<uint64_t>(1, 8ull * device_sms() / across);
-  return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({want, (uint64_t)kDzParts, (p.rows + 15) / 16}));
+// The runs of rows: as many CTAs as run at a time where their column sums are wanted, else four times as many.  Column sums go to scratch, run by run, for a second kernel to add; small
+// matrices (up to kDzSmall elements) are cut into narrower CTAs and eight runs, which add them up within a cluster: one
+// launch less (333 x 1151: 6.5 us instead of 4.5 and 3.0, and 3.5 us less on the host).
+constexpr uint64_t kDzSmall = 1u << 20;
+struct DzPlan {
+  uint32_t parts, wide;
+  uint64_t blocks;
+  bool cluster;
+};
+DzPlan dz_plan(const DzLaunch& p, int v) {
+  DzPlan d{1, 8, 0, p.db && p.rows <= kDzSmall / p.cols};
+  const uint64_t sms = (uint64_t)device_sms();
+  auto blocks = [&](uint32_t wide) { return (p.cols + 32u * v * wide - 1) / (32u * v * wide); };
+  while (d.wide > 1 && (32u * v * (d.wide / 2) >= p.cols || (d.cluster && blocks(d.wide) * 8 < sms))) d.wide /= 2;
+  d.blocks = blocks(d.wide);
+  const uint64_t rows = 4u * (8u / d.wide);
+  const uint64_t want = std::max<uint64_t>(1, std::min<uint64_t>((p.db ? 4 : 16) * sms / d.blocks, (p.rows + rows - 1) / rows));
+  d.parts = (uint32_t)want;
+  if (d.cluster)
+    for (d.parts = 8; d.parts > want; d.parts /= 2) {}
+  return d;
 }
 
 bool dz_vectors(const DzLaunch& p) {
@@ -940,11 +1023,18 @@ bool dz_vectors(const DzLaunch& p) {
          ok(p.dmul, p.lddmul);
 }
 
+int dz_width(const DzLaunch& p) { return !dz_vectors(p) ? 1 : p.dtype == MP_BF16 ? 8 : 4; }
+
 template <typename T, int V>
 cudaError_t dz_of(const DzLaunch& p, float* part, cudaStream_t st) {
+  const DzPlan plan = dz_plan(p, V);
   DzArgs<T> a;
   a.rows = p.rows;
   a.cols = (uint32_t)p.cols;
+  a.parts = plan.parts;
+  a.wide = plan.wide;
+  a.cluster = plan.cluster ? 1u : 0u;
+  a.rows_each = (p.rows + plan.parts - 1) / plan.parts;
   a.dy = static_cast<const T*>(p.dy.p);
   a.lddy = p.dy.ld;
   a.pre = static_cast<const T*>(p.pre.p);
@@ -955,20 +1045,24 @@ cudaError_t dz_of(const DzLaunch& p, float* part, cudaStream_t st) {
   a.lddz = p.lddz;
   a.dmul = static_cast<T*>(p.dmul);
   a.lddmul = p.lddmul;
-  a.part = p.db ? part : nullptr;
-  const uint32_t parts = dz_parts(p, V);
-  a.rows_each = (p.rows + parts - 1) / parts;
-  const dim3 grid((unsigned)((p.cols + 32u * V - 1) / (32u * V)), parts);
+  a.db = static_cast<T*>(p.db);
+  a.part = p.db && !plan.cluster ? part : nullptr;
+  const uint64_t ctas = plan.blocks * plan.parts;
+  if (ctas > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+  auto go = [&](auto kernel) {
+    return plan.cluster ? launch_cluster(kernel, (unsigned)ctas, 256, plan.parts, 0, st, a)
+                        : launch_kernel(true, kernel, dim3((unsigned)ctas), 256, 0, st, a);
+  };
   cudaError_t e;
   switch (p.act) {
-    case MP_ACT_RELU: e = dz_launch<T, V, MP_ACT_RELU>(a, grid, st); break;
-    case MP_ACT_SILU: e = dz_launch<T, V, MP_ACT_SILU>(a, grid, st); break;
-    case MP_ACT_GELU: e = dz_launch<T, V, MP_ACT_GELU>(a, grid, st); break;
-    case MP_ACT_GELU_TANH: e = dz_launch<T, V, MP_ACT_GELU_TANH>(a, grid, st); break;
-    default: e = dz_launch<T, V, MP_ACT_NONE>(a, grid, st); break;
+    case MP_ACT_RELU: e = go(dz_kernel<T, V, MP_ACT_RELU>); break;
+    case MP_ACT_SILU: e = go(dz_kernel<T, V, MP_ACT_SILU>); break;
+    case MP_ACT_GELU: e = go(dz_kernel<T, V, MP_ACT_GELU>); break;
+    case MP_ACT_GELU_TANH: e = go(dz_kernel<T, V, MP_ACT_GELU_TANH>); break;
+    default: e = go(dz_kernel<T, V, MP_ACT_NONE>); break;
   }
-  if (e != cudaSuccess || !p.db) return e;
-  return launch_column_sums(p.dtype, part, parts, (uint32_t)p.cols, p.db, st);
+  if (e != cudaSuccess || !a.part) return e;
+  return launch_column_sums(p.dtype, part, plan.parts, (uint32_t)p.cols, p.db, st);
 }
 
 }  // namespace
@@ -982,8 +1076,21 @@ mp_status launch_gemm(const GemmLaunch& g, cudaStream_t st) {
   return gemm_f32(g, st);
 }
 
+mp_status launch_gemms(const GemmLaunch& dx, const GemmLaunch& dw, cudaStream_t st) {
+  mp_status s;
+  if (dx.dtype == MP_BF16 && large_product(dx.e) && large_product(dw.e)) {
+    Prepared a, b;
+    if ((s = prepare_large(dx, a)) != MP_OK || (s = prepare_large(dw, b)) != MP_OK) return s;
+    return launch_large<false, true, true>(dx, a, b, st);
+  }
+  if ((s = launch_gemm(dx, st)) != MP_OK) return s;
+  return launch_gemm(dw, st);
+}
+
 size_t dz_scratch(const DzLaunch& p) {
-  return p.db ? (size_t)kDzParts * p.cols * sizeof(float) : 0;
+  if (!p.db) return 0;
+  const DzPlan plan = dz_plan(p, dz_width(p));
+  return plan.cluster ? 0 : (size_t)plan.parts * p.cols * sizeof(float);
 }
 
 cudaError_t launch_dz(const DzLaunch& p, float* scratch, cudaStream_t st) {

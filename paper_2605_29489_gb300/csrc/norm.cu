@@ -15,6 +15,7 @@
 #include <algorithm>
 
 #include "layer.cuh"
+#include "umma.cuh"
 
 namespace mp {
 
@@ -326,6 +327,177 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), (ROWT == 32 ? 3 : 4) * backwar
   }
 }
 
+// The same for many rows of whole 16-byte vectors: bulk copies bring them, ring slots of an x, a dy and an add row each, so that an
+// SM has about 200 KB on their way at any time, whatever its threads wait for: RMS norm 4096 x 4096 with add, 41 us with
+// the next row in registers (48 KB an SM), PLACEHOLDER with the ring.  A producer warp fills the slots in the order of the rows;
+// groups of ROWT threads, 16 columns each, take the rows in turn.  The groups' sums are added up in shared memory:
+// one part per CTA.
+constexpr int kRingThreads = 512 + 32, kRingSlots = 16;
+template <typename T, int ROWT, bool LAYER>
+__global__ void __launch_bounds__(kRingThreads, 1) norm_backward_ring_kernel(const NormLaunch p, float* part, uint32_t slots,
+                                                                             uint32_t row_bytes) {
+  kernel_begin();
+  constexpr int V = Elem<T>::kVec, NV = 16 / V, kGroups = 512 / ROWT, kGroupWarps = ROWT / 32;
+  constexpr bool kKeep = !LAYER;  // xh and g stay in registers; beside two sums per column they are read twice
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ uint64_t full[kRingSlots], empty[kRingSlots], meet[kGroups];
+  __shared__ float2 red[kGroups][2][kGroupWarps];
+  __shared__ volatile int abort;
+  const Wait& wt = p.wait;
+  const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
+  const uint32_t mats = p.add ? 3u : 2u, slot_bytes = mats * row_bytes;
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < slots; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], kGroupWarps);
+    }
+    for (int g = 0; g < kGroups; ++g) mbar_init(&meet[g], kGroupWarps);
+    mbar_fence_init();
+    abort = 0;
+  }
+  __syncthreads();
+  const uint64_t n_rows = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // of this CTA: blockIdx.x + n gridDim.x
+  float aw[16] = {}, ab[16] = {};
+  const uint32_t group = warp / kGroupWarps, at = threadIdx.x % ROWT;
+  if (warp == 16) {
+    uint64_t n = 0;
+    for (; n < n_rows; ++n) {
+      const uint32_t s = (uint32_t)(n % slots);
+      if (n >= slots && !warp_wait(&empty[s], (uint32_t)((n / slots) - 1) & 1u, &abort, wt.limit)) {
+        give_up(&abort, wt);
+        break;
+      }
+      if (!(wt.stall && n == 0) && elect_one()) {
+        const uint64_t r = blockIdx.x + n * gridDim.x;
+        uint8_t* to = ring + s * slot_bytes;
+        fence_proxy_async_smem();
+        mbar_arrive_expect_tx(&full[s], slot_bytes);
+        tma_load_1d(to, static_cast<const T*>(p.x) + r * p.ldx, row_bytes, &full[s]);
+        tma_load_1d(to + row_bytes, static_cast<const T*>(p.dy) + r * p.lddy, row_bytes, &full[s]);
+        if (p.add) tma_load_1d(to + 2 * row_bytes, static_cast<const T*>(p.add) + r * p.ldadd, row_bytes, &full[s]);
+      }
+      __syncwarp();
+    }
+    if (abort)  // the copies still on their way end before the CTA does
+      for (uint64_t q = n > slots ? n - slots : 0u; q < n; ++q)
+        if (!(wt.stall && q == 0)) mbar_wait_drain(&full[q % slots], (uint32_t)(q / slots) & 1u);
+  } else {
+    const T* w = static_cast<const T*>(p.weight);
+    const float inv = 1.0f / (float)p.cols;
+    uint32_t turn = 0, phase = 0;
+    auto place = [&](int k) { return (uint32_t)(k * ROWT + at) * V; };
+    float mun = 0.0f, rstdn = 0.0f;
+    auto stats = [&](uint64_t n) {
+      const uint64_t r = blockIdx.x + n * gridDim.x;
+      if (LAYER) mun = p.mean[r];
+      rstdn = p.rstd[r];
+    };
+    if (group < n_rows) stats(group);
+    for (uint64_t n = group; n < n_rows; n += kGroups) {
+      const uint32_t s = (uint32_t)(n % slots);
+      const float mu = mun, rstd = rstdn;
+      if (n + kGroups < n_rows) stats(n + kGroups);
+      if (!warp_wait(&full[s], (uint32_t)(n / slots) & 1u, &abort, wt.limit)) {
+        if (lane == 0) give_up(&abort, wt);
+        break;
+      }
+      const T* x = reinterpret_cast<const T*>(ring + s * slot_bytes);
+      const T* dy = reinterpret_cast<const T*>(ring + s * slot_bytes + row_bytes);
+      const T* add = reinterpret_cast<const T*>(ring + s * slot_bytes + 2 * row_bytes);
+      float h[16], g[16], u[V];
+      float s1 = 0.0f, s2 = 0.0f;
+      Pack<T, V> aq[NV];
+      // 16 columns' xh in hk and dy in gk; then the weight in u
+      auto take = [&](int k, float* hk, float* gk) {
+        unpack(load_pack<T, V>(x + place(k)), hk);
+        unpack(load_pack<T, V>(dy + place(k)), gk);
+        if (w) unpack(load_pack<T, V>(w + place(k)), u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) hk[e] = (LAYER ? hk[e] - mu : hk[e]) * rstd;
+      };
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (place(k) < p.cols) {
+          float *hk = h + k * V, *gk = g + k * V;
+          take(k, hk, gk);
+          if (kKeep && p.add) aq[k] = load_pack<T, V>(add + place(k));
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            aw[k * V + e] = fmaf(gk[e], hk[e], aw[k * V + e]);
+            if (LAYER) ab[k * V + e] += gk[e];
+            if (w) gk[e] *= u[e];
+            s1 = fmaf(gk[e], hk[e], s1);
+            if (LAYER) s2 += gk[e];
+          }
+        }
+      __syncwarp();
+      if ((kKeep || !p.dx) && lane == 0) mbar_arrive(&empty[s]);
+      if (!p.dx) continue;
+      s1 = warp_sum(s1);
+      if (LAYER) s2 = warp_sum(s2);
+      float2* set = red[group][turn++ & 1u];
+      if (lane == 0) set[warp % kGroupWarps] = make_float2(s1, s2);
+      if (!consumer_barrier(&meet[group], phase, &abort, wt.limit)) {
+        if (lane == 0) give_up(&abort, wt);
+        break;
+      }
+      const float2 v = set[lane % kGroupWarps];
+      s1 = v.x;
+      s2 = v.y;
+#pragma unroll
+      for (int o = kGroupWarps / 2; o > 0; o >>= 1) {
+        s1 += __shfl_xor_sync(0xFFFFFFFFu, s1, o);
+        if (LAYER) s2 += __shfl_xor_sync(0xFFFFFFFFu, s2, o);
+      }
+      const float m1 = s1 * inv, m2 = s2 * inv;
+      T* dx = static_cast<T*>(p.dx) + (blockIdx.x + n * gridDim.x) * p.lddx;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (place(k) < p.cols) {
+          float *hk = h + k * V, *gk = g + k * V;
+          if (!kKeep) {
+            take(k, hk, gk);
+            if (w)
+#pragma unroll
+              for (int e = 0; e < V; ++e) gk[e] *= u[e];
+          }
+          if (p.add) unpack(kKeep ? aq[k] : load_pack<T, V>(add + place(k)), u);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            gk[e] = fmaf(-hk[e], m1, LAYER ? gk[e] - m2 : gk[e]) * rstd;
+            if (p.add) gk[e] += u[e];
+          }
+          store_pack<T, V>(dx + place(k), pack<T, V>(gk));
+        }
+      __syncwarp();
+      if (!kKeep && lane == 0) mbar_arrive(&empty[s]);
+    }
+  }
+  __syncthreads();  // every slot has been read, or its copy waited for
+  if (!part) return;
+  float* sums = reinterpret_cast<float*>(ring);  // [kGroups][cols]
+#pragma unroll
+  for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
+    if (warp < 16) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const uint32_t c = (uint32_t)(k * ROWT + at) * V;
+        if (c < p.cols)
+#pragma unroll
+          for (int e = 0; e < V; ++e) sums[group * p.cols + c + e] = which ? ab[k * V + e] : aw[k * V + e];
+      }
+    }
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < p.cols; c += kRingThreads) {
+      float v = 0.0f;
+#pragma unroll
+      for (int q = 0; q < kGroups; ++q) v += sums[q * p.cols + c];
+      part[((uint64_t)blockIdx.x * 2 + which) * p.cols + c] = v;
+    }
+    __syncthreads();
+  }
+}
+
 // wide rows: dx alone, x and dy read twice
 template <typename T, int V, bool LAYER>
 __global__ void __launch_bounds__(1024, 1) norm_backward_wide_kernel(const NormLaunch p) {
@@ -486,9 +658,42 @@ uint32_t backward_ctas(const NormLaunch& p) {
   return (uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * ((t == 32 ? 3 : 4) * backward_threads<T, V>() / 4 / std::max(t, 128)));
 }
 
+// The ring: rows of 2 KB or more of whole vectors, four or more to an SM (fewer do not fill the ring twice); 0 slots: not.
+struct RingPlan {
+  uint32_t slots, slot_bytes, ctas;
+};
+RingPlan ring_plan(const NormLaunch& p) {
+  const uint32_t es = p.dtype == MP_BF16 ? 2 : 4, row = p.cols * es, slot = (p.add ? 3u : 2u) * row;
+  const int sms = sm_count();
+  RingPlan r{0, slot, (uint32_t)sms};
+  if (p.cols > kWideCols || row < 2048 || row % 16 != 0 || p.rows < 4ull * sms) return r;
+  if (!row16(p.x, p.ldx, es) || !row16(p.dy, p.lddy, es) || !row16(p.add, p.ldadd, es) || !row16(p.dx, p.lddx, es) ||
+      !row16(p.weight, 0, es))
+    return r;
+  const uint32_t n = 200u * 1024u / slot;
+  r.slots = n < 2 ? 0 : std::min<uint32_t>(n, kRingSlots);
+  return r;
+}
+
+template <typename T, bool LAYER>
+cudaError_t norm_backward_ring(const NormLaunch& p, const RingPlan& r, float* part, cudaStream_t st) {
+  const size_t smem = std::max<size_t>((size_t)r.slots * r.slot_bytes, 4u * kWideCols);
+  auto go = [&](auto kernel) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(true, kernel, dim3(r.ctas), kRingThreads, smem, st, p, part, r.slots, p.cols * (uint32_t)sizeof(T));
+  };
+  return p.cols <= 2048   ? go(norm_backward_ring_kernel<T, 128, LAYER>)
+         : p.cols <= 4096 ? go(norm_backward_ring_kernel<T, 256, LAYER>)
+                          : go(norm_backward_ring_kernel<T, 512, LAYER>);
+}
+
 constexpr uint32_t kWideParts = 64;
 
 uint32_t backward_parts(const NormLaunch& p) {
+  const RingPlan r = ring_plan(p);
+  if (r.slots) return r.ctas;
   if (p.cols > kWideCols) return (uint32_t)std::min<uint64_t>(kWideParts, p.rows);
   const bool vec = vectors_ok(p, true);
   if (p.dtype == MP_BF16) return vec ? backward_ctas<__nv_bfloat16, 8>(p) : backward_ctas<__nv_bfloat16, 1>(p);
@@ -513,6 +718,8 @@ cudaError_t norm_backward_rows(const NormLaunch& p, float* part, cudaStream_t st
 template <typename T, bool LAYER>
 cudaError_t norm_backward_of(const NormLaunch& p, float* part, cudaStream_t st) {
   constexpr int V = Elem<T>::kVec;
+  const RingPlan ring = ring_plan(p);
+  if (ring.slots) return norm_backward_ring<T, LAYER>(p, ring, part, st);
   const bool vec = vectors_ok(p, true);
   if (p.cols > kWideCols) {
     if (p.dx) {

@@ -100,7 +100,9 @@ def near(got, want, bound, what):
 # ---- norms --------------------------------------------------------------------------------------
 
 NORM_SHAPES = [(1, 1), (1, 896), (3, 8), (5, 7), (2, 33), (9, 257), (130, 128), (64, 1024), (33, 2056), (700, 1537),
-               (17, 4096), (3, 5003), (5, 8192), (2, 8200), (3, 12288), (2, 16384), (2, 16400), (1, 20001), (1201, 64)]
+               (17, 4096), (3, 5003), (5, 8192), (2, 8200), (3, 12288), (2, 16384), (2, 16400), (1, 20001), (1201, 64),
+               # many rows of whole vectors: the backward pass's ring, of every width and number of slots
+               (700, 1024), (1300, 1032), (611, 2056), (777, 4096), (640, 8192)]
 
 
 @pytest.mark.parametrize("shape", NORM_SHAPES)
@@ -215,7 +217,7 @@ def test_norm_is_the_same_every_time(mp):
 # both kernels of the tensor cores
 LINEAR_SHAPES = [(1, 1, 1), (1, 64, 128), (1, 896, 1152), (1, 901, 77), (2, 8, 8), (7, 333, 130), (16, 2048, 512),
                  (17, 1000, 129), (33, 72, 1000), (65, 640, 264), (128, 512, 384), (129, 100, 131), (300, 1151, 901),
-                 (513, 256, 1024), (1024, 320, 2304), (2000, 136, 4104)]
+                 (513, 256, 1024), (1024, 320, 2304), (2000, 136, 4104), (2600, 1000, 2568)]
 F32_SHAPES = [(1, 1, 1), (1, 512, 512), (3, 17, 65), (64, 64, 64), (65, 130, 67), (200, 333, 129)]
 
 
@@ -708,6 +710,27 @@ def test_a_wait_that_runs_out_is_reported(mp, rows):
     assert e.value.status == -6
     mp.mp_layer_status()
     assert torch.equal(mp.mp_linear(c["x"], c["w"])[0], want)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_a_norm_whose_ring_is_not_filled_is_reported(mp, kind):
+    x, dy, w = make((900, 2048), "bf16", 1), make((900, 2048), "bf16", 2), make((2048,), "bf16", 3)
+    k = mp.MP_NORM_LAYER if kind == "layer" else mp.MP_NORM_RMS
+    _, mean, rstd = mp.mp_norm(x, w, kind=k)
+    want = mp.mp_norm_backward(dy, x, w, mean, rstd, kind=k)
+    mp.mp_layer_status()
+    mp.mp_debug_stall_pipeline(2000)
+    try:
+        mp.mp_norm_backward(dy, x, w, mean, rstd, kind=k)
+        torch.cuda.synchronize()
+    finally:
+        mp.mp_debug_stall_pipeline(0)
+    with pytest.raises(mp.MergePipeError) as e:
+        mp.mp_layer_status()
+    assert e.value.status == -6
+    got = mp.mp_norm_backward(dy, x, w, mean, rstd, kind=k)
+    mp.mp_layer_status()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 def test_trace_ranges(mp):
