@@ -262,7 +262,7 @@ __device__ __forceinline__ bool warp_wait_cluster(uint64_t* bar, uint32_t parity
 // Few rows.  out[r, c]: c (features, the lanes of tensor memory) from operand a, r from operand b.  A cluster makes one
 // tile of 128 c x BN r; its CTA q has the q-th part of the inner dimension.  Tiles with the same features are neighbours.
 template <int BN, bool AT, bool BT>
-__global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_constant__ CUtensorMap ma,
+__global__ void __launch_bounds__(kGemmThreads, 4) split_kernel(const __grid_constant__ CUtensorMap ma,
                                                              const __grid_constant__ CUtensorMap mb, const Epi<bf16> e,
                                                              uint32_t kb_all, uint32_t tiles_r, int stages, const Wait w) {
   constexpr int kMaxStages = 12;
@@ -338,6 +338,14 @@ __global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_consta
     if (elect_one()) umma_commit<1>(&done);
     mbar_wait_drain(&done, 0);
   }
+  // the rest of the warps: what the epilogue will read is brought to L2 meanwhile, then the products' end
+  const uint32_t n_r = min((uint32_t)BN, e.rows - (uint32_t)r0), j1 = n_r * (rank + 1) / split;
+  if (warp >= 2 && (e.mul || e.res))
+    for (uint32_t j = n_r * rank / split + warp - 2; j < j1; j += 4) {
+      const uint32_t at = (uint32_t)c0 + lane * 4u;
+      if (at < e.cols && e.mul) prefetch_l2(e.mul + (r0 + (uint64_t)j) * e.ldmul + at);
+      if (at < e.cols && e.res) prefetch_l2(e.res + (r0 + (uint64_t)j) * e.ldres + at);
+    }
   __syncwarp();
   const bool ok = warp < 2 || warp_wait(&done, 0, &abort, w.limit);
   if (!ok && lane == 0) give_up(&abort, w);
@@ -345,7 +353,6 @@ __global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_consta
   umma_fence_after();
   // the CTA's sums to shared memory, [rows][128] (the stages are over), then every warp takes whole rows: a lane's
   // four features from each CTA in turn, several rows' loads in flight
-  const uint32_t n_r = min((uint32_t)BN, e.rows - (uint32_t)r0);
   if (warp >= 2) {
     const uint32_t quarter = warp & 3u, row = quarter * 32u + lane;  // this thread's lane of tensor memory
 #pragma unroll 1
@@ -367,33 +374,38 @@ __global__ void __launch_bounds__(kGemmThreads) split_kernel(const __grid_consta
 #pragma unroll
     for (int k = 0; k < 4; ++k) bias[k] = c + k < e.cols ? epi_bias(e, c + k) : 0.0f;
     const bool whole = e.quad && c + 4 <= e.cols;
-    const uint32_t j1 = n_r * (rank + 1) / split;
-    constexpr int kAhead = 4;
-    for (uint32_t j = n_r * rank / split + warp; j < j1; j += kWarps * kAhead) {
-      float4 z[kAhead];
+    // S CTAs' sums of 8 / S rows at a time: eight loads of a lane in flight
+    auto add_up = [&](auto of) {
+      constexpr int S = decltype(of)::value, kAhead = 8 / S;
+      for (uint32_t j = n_r * rank / S + warp; j < j1; j += kWarps * kAhead) {
+        float4 u[kAhead][S];
 #pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        z[a] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const uint32_t at = smem + (min(j + a * kWarps, j1 - 1) * 128u + lane * 4u) * 4u;
-        if (split == 1) {
-          z[a] = cluster_load4(at);
-        } else {
-          for (uint32_t q = 0; q < split; q += 2) {
-            const float4 u = cluster_load4(cluster_map(at, q)), v = cluster_load4(cluster_map(at, q + 1));
-            z[a].x = (z[a].x + u.x) + v.x;
-            z[a].y = (z[a].y + u.y) + v.y;
-            z[a].z = (z[a].z + u.z) + v.z;
-            z[a].w = (z[a].w + u.w) + v.w;
+        for (int a = 0; a < kAhead; ++a) {
+          const uint32_t at = smem + (min(j + a * kWarps, j1 - 1) * 128u + lane * 4u) * 4u;
+#pragma unroll
+          for (int q = 0; q < S; ++q) u[a][q] = cluster_load4(S == 1 ? at : cluster_map(at, q));
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+          if (j + a * kWarps < j1) {
+            float v[4] = {u[a][0].x, u[a][0].y, u[a][0].z, u[a][0].w};
+#pragma unroll
+            for (int q = 1; q < S; ++q) {
+              v[0] += u[a][q].x;
+              v[1] += u[a][q].y;
+              v[2] += u[a][q].z;
+              v[3] += u[a][q].w;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] += bias[k];
+            epi_quad(e, (uint32_t)r0 + j + a * kWarps, c, v, whole);
           }
-        }
       }
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a)
-        if (j + a * kWarps < j1) {
-          float v[4] = {z[a].x + bias[0], z[a].y + bias[1], z[a].z + bias[2], z[a].w + bias[3]};
-          epi_quad(e, (uint32_t)r0 + j + a * kWarps, c, v, whole);
-        }
-    }
+    };
+    if (split == 1) add_up(std::integral_constant<int, 1>());
+    if (split == 2) add_up(std::integral_constant<int, 2>());
+    if (split == 4) add_up(std::integral_constant<int, 4>());
+    if (split == 8) add_up(std::integral_constant<int, 8>());
   }
   if (split > 1) cluster_sync();  // nothing of this CTA is read any more
   umma_fence_before();
