@@ -1,0 +1,124 @@
+"""Learning merge coefficients from what the merged layer computes.
+
+A gated feed-forward block (RMS norm, SiLU gate, up and down projection, residual) of a small language
+model's sizes is merged from a base and K experts by task arithmetic under a read budget.  The coefficients are not
+given: they start at zero, and each step
+
+    plan -> merge -> the block's forward pass on calibration tokens -> loss -> backward pass -> gradient of the coefficients
+
+moves them down the loss against a teacher's outputs, here those of a hidden mixture of the same experts (random
+weights and tokens: there is nothing to download).  All of it runs through the package's calls; torch holds the
+memory and does the loss.
+
+    python examples/learn_coefficients.py [--steps 60] [--tokens 512] [--budget 1.0]
+"""
+import argparse
+import os
+import sys
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+import torch  # noqa: E402
+
+import paper_2605_29489_gb300 as mp  # noqa: E402
+
+HIDDEN, INNER, BLOCK = 896, 4864, 65536
+SHAPES = {"norm": (HIDDEN,), "gate": (INNER, HIDDEN), "up": (INNER, HIDDEN), "down": (HIDDEN, INNER)}
+
+
+def layout():
+    """{name: (offset, elements)} in one flat checkpoint, every tensor on a 16-byte boundary"""
+    at, places = 0, {}
+    for name, shape in SHAPES.items():
+        n = int(torch.Size(shape).numel())
+        places[name] = (at, n)
+        at += (n + 7) // 8 * 8
+    return places, at
+
+
+def views(flat, places):
+    return {name: flat[o:o + n].view(SHAPES[name]) for name, (o, n) in places.items()}
+
+
+def forward(w, x):
+    """the block's output, and what its backward pass needs"""
+    n, _, rstd = mp.mp_norm(x, w["norm"])
+    up, _ = mp.mp_linear(n, w["up"])
+    h, pre = mp.mp_linear(n, w["gate"], act=mp.MP_ACT_SILU, mul=up, keep_pre=True)
+    y, _ = mp.mp_linear(h, w["down"], residual=x)
+    return y, (n, rstd, up, h, pre)
+
+
+def backward(w, g, x, kept, dy):
+    """the gradient of every weight into the views g of one flat buffer, and that of x"""
+    n, rstd, up, h, pre = kept
+    dh, _, _, _ = mp.mp_linear_backward(dy, h, w["down"], dw=g["down"])
+    dn, _, _, dup = mp.mp_linear_backward(dh, n, w["gate"], pre=pre, act=mp.MP_ACT_SILU, mul=up, dw=g["gate"])
+    dn, _, _, _ = mp.mp_linear_backward(dup, n, w["up"], dx_add=dn, dx=dn, dw=g["up"])
+    dx, dnorm, _ = mp.mp_norm_backward(dn, x, w["norm"], None, rstd, add=dy)
+    g["norm"].copy_(dnorm)
+    return dx
+
+
+def family(K, seed):
+    """a base and K experts, each different from the base on half of its blocks"""
+    places, total = layout()
+    rnd = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda n: torch.randn(n, generator=rnd, device="cuda")  # noqa: E731
+    base = normal(total) * 0.02
+    base[places["norm"][0]:places["norm"][0] + HIDDEN] += 1.0
+    experts = []
+    for _ in range(K):
+        blocks = torch.rand((total + BLOCK - 1) // BLOCK, generator=rnd, device="cuda") < 0.5
+        experts.append((base + normal(total) * 0.01 * blocks.repeat_interleave(BLOCK)[:total]).bfloat16())
+    base = base.bfloat16()
+    return mp.family([places[n] for n in SHAPES], base, experts, BLOCK), places, rnd
+
+
+def learn(K=4, steps=60, tokens=512, budget=1.0, rate=0.1, seed=0, report=None):
+    """(coefficients, the teacher's, losses)"""
+    fam, places, rnd = family(K, seed)
+    index = mp.mp_index_blocks(fam)
+    teacher = [0.6, -0.3, 0.4, 0.2] * ((K + 3) // 4)
+    teacher = teacher[:K]
+    merged, grad = torch.empty_like(fam.base), torch.zeros_like(fam.base)
+    w, g = views(merged, places), views(grad, places)
+    x = torch.randn((tokens, HIDDEN), generator=rnd, device="cuda").bfloat16()
+
+    def merge(alpha, fraction):
+        op = mp.make_op(mp.MP_OP_TA, alpha=alpha)
+        plan = mp.mp_plan(index, op, mp.mp_budget_from_fraction(fam, fraction))
+        mp.mp_merge(fam, index, plan, merged).free()
+        return plan
+
+    merge(teacher, 1.0).free()
+    goal = forward(w, x)[0].float()
+
+    alpha = torch.zeros(K, dtype=torch.float64)
+    mean, square, losses = torch.zeros_like(alpha), torch.zeros_like(alpha), []
+    for step in range(1, steps + 1):
+        plan = merge(alpha.tolist(), budget)
+        y, kept = forward(w, x)
+        off = y.float() - goal
+        losses.append(off.square().mean().item())
+        backward(w, g, x, kept, (off * (2.0 / off.numel())).bfloat16())
+        slope = mp.mp_coef_grad(fam, index, plan, grad).sum(1).double().cpu()  # over the tensors: one alpha per expert
+        plan.free()
+        mean, square = 0.8 * mean + 0.2 * slope, 0.95 * square + 0.05 * slope.square()  # Adam, the rate falling to a tenth
+        step_size = rate * 0.1 ** (step / steps)
+        alpha -= step_size * (mean / (1 - 0.8 ** step)) / ((square / (1 - 0.95 ** step)).sqrt() + 1e-30)
+        if report and (step == 1 or step % 10 == 0):
+            report(f"step {step:3d}  loss {losses[-1]:.3e}  alpha {[round(a, 3) for a in alpha.tolist()]}")
+    index.free()
+    mp.mp_layer_status()
+    return alpha.tolist(), teacher, losses
+
+
+if __name__ == "__main__":
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--steps", type=int, default=60)
+    ap.add_argument("--tokens", type=int, default=512)
+    ap.add_argument("--budget", type=float, default=1.0, help="fraction of the full expert read")
+    a = ap.parse_args()
+    found, hidden, losses = learn(steps=a.steps, tokens=a.tokens, budget=a.budget, report=print)
+    print(f"loss {losses[0]:.3e} -> {losses[-1]:.3e}, coefficients {[round(v, 3) for v in found]}, the teacher's {hidden}")

@@ -493,7 +493,7 @@ mp_status mp_linear_backward(const mp_linear_backward_args* args, mp_stream stre
  * gradients are taken straight through the rounding of the merged weights.  out: device, fp32
  * [K][n_tensors].  The plan's operator must be AVG or TA (MP_ERR_UNSUPPORTED for the others, whose
  * output is not linear in alpha), the experts in device memory (MP_ERR_UNSUPPORTED for a host-resident pool).  Sums: fp32
- * within 16 KiB of a block, fp64 over those, in a fixed order.
+ * within 32 KiB of a block, fp64 over those, in a fixed order.
  * Errors: MP_ERR_INVALID_ARG, MP_ERR_MISMATCH, MP_ERR_UNSUPPORTED, MP_ERR_OOM, MP_ERR_CUDA.
  */
 mp_status mp_coef_grad(const mp_family* family, const mp_index* index, const mp_plan_t* plan, const void* grad,

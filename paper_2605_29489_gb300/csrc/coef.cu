@@ -18,8 +18,8 @@ namespace mp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kVecs = 4;                                     // vectors a thread keeps at a time
-constexpr uint32_t kItemVecs = kThreads * kVecs * 2;         // an item: two rounds of those
+constexpr int kVecs = 2;                              // vectors a thread keeps at a time
+constexpr uint32_t kItemVecs = kThreads * kVecs * 4;  // an item: four rounds of those
 
 template <typename T>
 constexpr uint32_t item_elems() {
@@ -54,7 +54,7 @@ __device__ __forceinline__ uint4 load_vec(const T* p, uint32_t v, uint32_t n) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) coef_kernel(const CoefLaunch p, float* part, uint32_t per_block) {
+__global__ void __launch_bounds__(kThreads, 4) coef_kernel(const CoefLaunch p, float* part, uint32_t per_block) {
   kernel_begin();
   constexpr int V = Elem<T>::kVec;
   __shared__ float sum[kThreads / 32][kMaxK];
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kThreads) coef_kernel(const CoefLaunch p, floa
 #pragma unroll
           for (int e = 0; e < V; ++e)
             a[k] = fmaf(elem_of<T>(g[k], e), elem_of<T>(x[k], e) - elem_of<T>(m[k], e), a[k]);
-        float s = (a[0] + a[1]) + (a[2] + a[3]);
+        float s = a[0] + a[1];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
         if (lane == 0) sum[warp][i] += s;
@@ -122,24 +122,27 @@ __global__ void __launch_bounds__(kThreads) coef_kernel(const CoefLaunch p, floa
   }
 }
 
-// out[i][t] = the sum of tensor t's items of expert i, in fp64: every thread a strided run, then a tree
+// out[i][t] = the sum of tensor t's items of expert i, in fp64: every thread a strided run, then a tree over lanes and
+// one over warps
 __global__ void __launch_bounds__(kThreads) coef_sum_kernel(const float* part, uint64_t n_items, uint32_t per_block,
                                                             const uint32_t* t_blk0, uint32_t n_tensors, float* out) {
   kernel_begin();
-  __shared__ double red[kThreads];
-  const uint32_t t = blockIdx.x, i = blockIdx.y;
+  __shared__ double red[kThreads / 32];
+  const uint32_t t = blockIdx.x, i = blockIdx.y, lane = threadIdx.x & 31u;
   const float* src = part + (uint64_t)i * n_items;
   double s = 0.0;
   for (uint64_t q = (uint64_t)t_blk0[t] * per_block + threadIdx.x; q < (uint64_t)t_blk0[t + 1] * per_block; q += kThreads)
     s += (double)src[q];
-  red[threadIdx.x] = s;
-  __syncthreads();
 #pragma unroll
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    if (threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-    __syncthreads();
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  if (lane == 0) red[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    s = lane < kThreads / 32 ? red[lane] : 0.0;
+#pragma unroll
+    for (int o = kThreads / 64; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (lane == 0) out[(uint64_t)i * n_tensors + t] = (float)s;
   }
-  if (threadIdx.x == 0) out[(uint64_t)i * n_tensors + t] = (float)red[0];
 }
 
 uint32_t items_per_block(const CoefLaunch& p) {

@@ -227,7 +227,8 @@ struct DzLaunch {
   void* db;
 };
 size_t dz_scratch(const DzLaunch& p);
-cudaError_t launch_dz(const DzLaunch& p, float* scratch, cudaStream_t st);
+// with n copies (two at most) in the same launch
+cudaError_t launch_dz(const DzLaunch& p, const Copy* copies, int n, float* scratch, cudaStream_t st);
 // the sum over n_part rows of part [n_part][cols] into out: the second step of every column sum here
 cudaError_t launch_column_sums(mp_dtype dtype, const float* part, uint32_t n_part, uint32_t cols, void* out,
                                cudaStream_t st);

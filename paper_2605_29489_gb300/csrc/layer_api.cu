@@ -106,8 +106,8 @@ mp_status norm_shape(mp_dtype dtype, mp_norm_kind kind, uint64_t rows, uint64_t 
 cudaStream_t stream_of(mp_stream s) { return reinterpret_cast<cudaStream_t>(s); }
 
 // Operands that the tensor cores cannot read as they are (a bf16 matrix whose rows are not whole 16-byte vectors)
-// are copied to scratch, with rows that are.  need() takes note of one, copy() makes the copies and points the
-// operands at them.
+// are copied to scratch, with rows that are.  need() takes note of one; place() points the operands at the copies, which
+// the caller then has made.
 struct Repack {
   Copy c[2];
   Mat* m[2];
@@ -121,12 +121,11 @@ struct Repack {
     m[n] = &x;
     at[n++] = s.plan(rows * ld * 2);
   }
-  cudaError_t copy(mp_dtype dtype, const Scratch& s, cudaStream_t cs) {
+  void place(const Scratch& s) {
     for (int k = 0; k < n; ++k) {
       c[k].dst = s.at(at[k]);
       *m[k] = Mat{c[k].dst, c[k].ldd};
     }
-    return n ? launch_copies(dtype, c, n, cs) : cudaSuccess;
   }
 };
 
@@ -278,7 +277,8 @@ mp_status linear(const mp_linear_args& a, mp_stream stream) {
   re.need(a.dtype, g.b, a.out, a.in, s);
   cudaError_t e;
   if ((e = s.get(cs)) != cudaSuccess) return cuda_fail(e, "scratch");
-  if ((e = re.copy(a.dtype, s, cs)) != cudaSuccess) return cuda_fail(e, "copy kernel");
+  re.place(s);
+  if (re.n && (e = launch_copies(a.dtype, re.c, re.n, cs)) != cudaSuccess) return cuda_fail(e, "copy kernel");
   g.inner = a.in;
   g.e = Epilogue{a.rows, a.out, a.bias, a.act, Mat{a.mul.data, a.mul.ld}, Mat{a.residual.data, a.residual.ld},
                  a.y.data, a.pre.data, a.y.ld, a.pre.ld};
@@ -361,9 +361,12 @@ mp_status linear_backward(const mp_linear_backward_args& a, mp_stream stream) {
     d.dz = s.at(dz_at);
     dz = Mat{d.dz, d.lddz};
   }
-  if ((own_dz || a.db || a.dmul.data) && (e = launch_dz(d, static_cast<float*>(s.at(part_at)), cs)) != cudaSuccess)
-    return cuda_fail(e, "linear kernel");
-  if ((e = re.copy(a.dtype, s, cs)) != cudaSuccess) return cuda_fail(e, "copy kernel");
+  re.place(s);
+  if (own_dz || a.db || a.dmul.data)
+    e = launch_dz(d, re.c, re.n, static_cast<float*>(s.at(part_at)), cs);
+  else if (re.n)
+    e = launch_copies(a.dtype, re.c, re.n, cs);
+  if (e != cudaSuccess) return cuda_fail(e, "linear kernel");
   g.a = dz;
   GemmLaunch g2 = g;
   if (a.dx.data) {

@@ -261,11 +261,17 @@ __device__ __forceinline__ bool warp_wait_cluster(uint64_t* bar, uint32_t parity
 
 // Few rows.  out[r, c]: c (features, the lanes of tensor memory) from operand a, r from operand b.  A cluster makes one
 // tile of 128 c x BN r; its CTA q has the q-th part of the inner dimension.  Tiles with the same features are neighbours.
+// A part of the inner dimension may be empty (short inner dimensions beside long ones in one launch): its sums are zeros.
+struct Split {
+  Epi<bf16> e;
+  uint32_t kb, tiles_r, stages;  // stages of the inner dimension; tiles down the rows; ring stages
+};
 template <int BN, bool AT, bool BT>
-__global__ void __launch_bounds__(kGemmThreads, 4) split_kernel(const __grid_constant__ CUtensorMap ma,
-                                                             const __grid_constant__ CUtensorMap mb, const Epi<bf16> e,
-                                                             uint32_t kb_all, uint32_t tiles_r, int stages, const Wait w) {
-  constexpr int kMaxStages = 12;
+__device__ __forceinline__ void split_tile(const CUtensorMap& ma, const CUtensorMap& mb, const Split& p, uint32_t block,
+                                           const Wait& w) {
+  const Epi<bf16>& e = p.e;
+  const uint32_t kb_all = p.kb, stages = p.stages;
+  constexpr int kMaxStages = 6;
   constexpr uint32_t kA = 128 * 128, kB = BN * 128, kStage = kA + kB;
   constexpr uint32_t kCols = BN < 32 ? 32 : BN;
   extern __shared__ uint8_t raw[];
@@ -276,11 +282,11 @@ __global__ void __launch_bounds__(kGemmThreads, 4) split_kernel(const __grid_con
   const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31u;
   uint32_t split, rank = cluster_rank();
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(split));
-  const uint32_t tile = blockIdx.x / split;
-  const int32_t r0 = (int32_t)(tile % tiles_r) * BN, c0 = (int32_t)(tile / tiles_r) * 128;
+  const uint32_t tile = block / split;
+  const int32_t r0 = (int32_t)(tile % p.tiles_r) * BN, c0 = (int32_t)(tile / p.tiles_r) * 128;
   const uint32_t k0 = (uint32_t)((uint64_t)kb_all * rank / split), k1 = (uint32_t)((uint64_t)kb_all * (rank + 1) / split);
   if (threadIdx.x == 0) {
-    for (int s = 0; s < stages; ++s) {
+    for (uint32_t s = 0; s < stages; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
@@ -301,7 +307,7 @@ __global__ void __launch_bounds__(kGemmThreads, 4) split_kernel(const __grid_con
     uint32_t it = 0;
     for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
       const uint32_t s = it % stages;
-      if (it >= (uint32_t)stages && !warp_wait(&empty[s], ((it / stages) - 1) & 1u, &abort, w.limit)) {
+      if (it >= stages && !warp_wait(&empty[s], ((it / stages) - 1) & 1u, &abort, w.limit)) {
         give_up(&abort, w);
         break;
       }
@@ -314,7 +320,7 @@ __global__ void __launch_bounds__(kGemmThreads, 4) split_kernel(const __grid_con
     }
     // the stages still on their way, when something gave up: their copies end before the CTA does
     if (abort)
-      for (uint32_t q = it > (uint32_t)stages ? it - stages : 0u; q < it; ++q)
+      for (uint32_t q = it > stages ? it - stages : 0u; q < it; ++q)
         if (!(w.stall && q == 0)) mbar_wait_drain(&full[q % stages], (q / stages) & 1u);
   } else if (warp == 1) {
     uint32_t it = 0;
@@ -357,8 +363,8 @@ __global__ void __launch_bounds__(kGemmThreads, 4) split_kernel(const __grid_con
     const uint32_t quarter = warp & 3u, row = quarter * 32u + lane;  // this thread's lane of tensor memory
 #pragma unroll 1
     for (uint32_t j0 = 0; j0 < n_r; j0 += 16) {
-      float v[16];
-      tmem_load16(tmem + ((quarter * 32u) << 16) + j0, v);
+      float v[16] = {};
+      if (k1 > k0) tmem_load16(tmem + ((quarter * 32u) << 16) + j0, v);
 #pragma unroll
       for (int j = 0; j < 16; ++j)
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + ((j0 + j) * 128u + row) * 4u), "f"(v[j]) : "memory");
@@ -411,6 +417,26 @@ __global__ void __launch_bounds__(kGemmThreads, 4) split_kernel(const __grid_con
   umma_fence_before();
   __syncthreads();
   if (warp == 1) tmem_free<1>(tmem, kCols);
+}
+
+template <int BN, bool AT, bool BT>
+__global__ void __launch_bounds__(kGemmThreads, 4) split_kernel(const __grid_constant__ CUtensorMap ma,
+                                                                const __grid_constant__ CUtensorMap mb, const Split p,
+                                                                const Wait w) {
+  split_tile<BN, AT, BT>(ma, mb, p, blockIdx.x, w);
+}
+
+// dx and dw of a small backward pass in one launch: dx's clusters first
+template <int BN>
+__global__ void __launch_bounds__(kGemmThreads, 4) split_two_kernel(const __grid_constant__ CUtensorMap ma,
+                                                                    const __grid_constant__ CUtensorMap mb, const Split p,
+                                                                    const __grid_constant__ CUtensorMap ma2,
+                                                                    const __grid_constant__ CUtensorMap mb2, const Split p2,
+                                                                    uint32_t blocks, const Wait w) {
+  if (blockIdx.x < blocks)
+    split_tile<BN, true, false>(ma, mb, p, blockIdx.x, w);
+  else
+    split_tile<128, true, true>(ma2, mb2, p2, blockIdx.x - blocks, w);
 }
 
 // A product of gemm_kernel: its maps are arguments of their own.
@@ -694,6 +720,35 @@ __global__ void __launch_bounds__(256, R == 1 ? 2 : 1) gemm_f32_kernel(const flo
 
 // ---- elementwise and layout kernels ---------------------------------------------------------------
 
+// copies (or zeros: no source) of matrices
+template <typename T>
+struct CopyArgs {
+  const T* src;
+  T* dst;
+  uint64_t lds, ldd, rows;
+  uint32_t cols;
+};
+// block's share (of `blocks`) of a copy: a warp to a row, four elements of a lane in flight
+template <typename T>
+__device__ __forceinline__ void copy_rows(const CopyArgs<T>& m, uint32_t block, uint32_t blocks) {
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  for (uint64_t r = block * 8ull + warp; r < m.rows; r += blocks * 8ull)
+    for (uint32_t c = lane; c < m.cols; c += 128u) {
+      T v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = m.src && c + 32u * k < m.cols ? m.src[r * m.lds + c + 32u * k] : T(0.0f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + 32u * k < m.cols) m.dst[r * m.ldd + c + 32u * k] = v[k];
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) copy_kernel(const CopyArgs<T> a, const CopyArgs<T> b) {
+  kernel_begin();
+  copy_rows(a, blockIdx.x, gridDim.x);
+  copy_rows(b, blockIdx.x, gridDim.x);
+}
+
 template <typename T>
 struct DzArgs {
   uint64_t rows, rows_each, lddy, ldpre, ldmul, lddz, lddmul;
@@ -702,17 +757,26 @@ struct DzArgs {
   const T *dy, *pre, *mul;
   T *dz, *dmul, *db;
   float* part;  // [parts][cols] column sums where the parts are no cluster
+  // the CTAs from `blocks` on copy operands of the products that follow
+  uint32_t blocks;
+  CopyArgs<T> copy[2];
 };
 
 // A CTA has 32 V `wide` columns (wide: the warps side by side, 1 to 8) and a run of rows, 8 / wide rows at a time.  Four
 // CTAs to an SM hide what a row waits for better than more rows in flight with fewer: 4096 x 14336, SiLU, three
 // matrices read and one written, 82 us; two rows and three CTAs 94, two and two 114 (a copy of as many bytes takes 76).  The
 // column sums of warps, then of CTAs, are added in order.
-template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(256, 4) dz_kernel(const DzArgs<T> p) {
+// COPY: some CTAs copy instead.
+template <typename T, int V, int ACT, bool COPY>
+__global__ void __launch_bounds__(256, COPY ? 3 : 4) dz_kernel(const DzArgs<T> p) {
   kernel_begin();
   constexpr bool FAST = sizeof(T) == 2;
   __shared__ float sum[8][32 * V + 1], total[8 * 32 * V];
+  if (COPY && blockIdx.x >= p.blocks) {
+    copy_rows(p.copy[0], blockIdx.x - p.blocks, gridDim.x - p.blocks);
+    copy_rows(p.copy[1], blockIdx.x - p.blocks, gridDim.x - p.blocks);
+    return;
+  }
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, deep = 8u / p.wide;
   const uint32_t across = 32u * V * p.wide;
   // a cluster's CTAs are neighbours; else those with the same rows are
@@ -728,21 +792,25 @@ __global__ void __launch_bounds__(256, 4) dz_kernel(const DzArgs<T> p) {
       Pack<T, V> zq, mq;
       if (p.pre) zq = load_pack<T, V>(p.pre + r * p.ldpre + c);
       if (p.mul) mq = load_pack<T, V>(p.mul + r * p.ldmul + c);
-      float d[V], z[V] = {}, m[V], om[V];
+      float d[V], z[V] = {};
       unpack(dq, d);
       if (p.pre) unpack(zq, z);
-      if (p.mul) unpack(mq, m);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         float a, g;
         act_both<ACT, FAST, true>(z[k], a, g);
-        om[k] = d[k] * a;
+        z[k] = d[k] * a;
         if (ACT != MP_ACT_NONE) d[k] *= g;
-        if (p.mul) d[k] *= m[k];
-        s[k] += d[k];
       }
+      if (p.dmul) store_pack<T, V>(p.dmul + r * p.lddmul + c, pack<T, V>(z));
+      if (p.mul) {
+        unpack(mq, z);
+#pragma unroll
+        for (int k = 0; k < V; ++k) d[k] *= z[k];
+      }
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[k] += d[k];
       if (p.dz) store_pack<T, V>(p.dz + r * p.lddz + c, pack<T, V>(d));
-      if (p.dmul) store_pack<T, V>(p.dmul + r * p.lddmul + c, pack<T, V>(om));
     }
   }
   if (!p.db) return;
@@ -764,31 +832,6 @@ __global__ void __launch_bounds__(256, 4) dz_kernel(const DzArgs<T> p) {
       p.db[c0 + k] = Elem<T>::store(v);
     }
   cluster_sync();
-}
-
-// copies (or zeros: no source) of up to two matrices, blockIdx.y saying which
-template <typename T>
-struct CopyArgs {
-  const T* src;
-  T* dst;
-  uint64_t lds, ldd, rows;
-  uint32_t cols;
-};
-template <typename T>
-__global__ void __launch_bounds__(256) copy_kernel(const CopyArgs<T> a, const CopyArgs<T> b) {
-  kernel_begin();
-  const CopyArgs<T>& m = blockIdx.y ? b : a;
-  // a warp to a row, four elements of a lane in flight
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  for (uint64_t r = blockIdx.x * 8ull + warp; r < m.rows; r += gridDim.x * 8ull)
-    for (uint32_t c = lane; c < m.cols; c += 128u) {
-      T v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = m.src && c + 32u * k < m.cols ? m.src[r * m.lds + c + 32u * k] : T(0.0f);
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (c + 32u * k < m.cols) m.dst[r * m.ldd + c + 32u * k] = v[k];
-    }
 }
 
 // ---- launches -------------------------------------------------------------------------------------
@@ -886,25 +929,9 @@ cudaError_t launch_cluster(void (*k)(P...), unsigned grid, unsigned threads, uns
   return cudaLaunchKernelEx(&cfg, k, P(a)...);
 }
 
-template <int BN, bool AT, bool BT>
-cudaError_t launch_split(const CUtensorMap& ma, const CUtensorMap& mb, const Epi<bf16>& e, uint32_t kb, unsigned split,
-                         int stages, const Wait& w, cudaStream_t st) {
-  const uint32_t tiles_r = (e.rows + BN - 1) / BN, tiles_c = (e.cols + 127u) / 128u;
-  // the stages, and in their place the sums at the end ([BN][128] fp32)
-  const size_t smem = std::max((size_t)stages * (128 * 128 + BN * 128), (size_t)BN * 512) + 1024;
-  return launch_cluster(split_kernel<BN, AT, BT>, tiles_r * tiles_c * split, kGemmThreads, split, smem, st, ma, mb, e, kb, tiles_r,
-                        stages, w);
-}
-
-template <bool AT, bool BT>
-cudaError_t launch_split_of(int bn, const CUtensorMap& ma, const CUtensorMap& mb, const Epi<bf16>& e, uint32_t kb,
-                            unsigned split, int stages, const Wait& w, cudaStream_t st) {
-  if constexpr (!BT) {
-    if (bn == 16) return launch_split<16, AT, BT>(ma, mb, e, kb, split, stages, w, st);
-    if (bn == 32) return launch_split<32, AT, BT>(ma, mb, e, kb, split, stages, w, st);
-    if (bn == 64) return launch_split<64, AT, BT>(ma, mb, e, kb, split, stages, w, st);
-  }
-  return launch_split<128, AT, BT>(ma, mb, e, kb, split, stages, w, st);
+// shared memory of a split product: the stages, and in their place the sums at the end ([BN][128] fp32)
+size_t split_bytes(int bn, int stages) {
+  return std::max((size_t)stages * (128 * 128 + bn * 128), (size_t)bn * 512) + 1024;
 }
 
 struct Prepared {  // a bf16 product on its way to a launch
@@ -944,6 +971,40 @@ mp_status launch_large(const GemmLaunch& g, const Prepared& a, const Prepared& b
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
 
+struct SplitPlan {
+  CUtensorMap ma, mb;  // of the columns' operand (the lanes of tensor memory) and of the rows'
+  Split p;
+  int bn;  // rows of a tile
+  uint64_t tiles;
+};
+
+mp_status prepare_split(const GemmLaunch& g, SplitPlan& q) {
+  q.bn = 128;
+  if (!g.a_t) q.bn = g.e.rows <= 16 ? 16 : g.e.rows <= 32 ? 32 : g.e.rows <= 64 ? 64 : 128;
+  mp_status s;
+  if ((s = make_map(&q.ma, g.b, g.b_t, g.e.cols, g.inner, 128u)) != MP_OK) return s;
+  if ((s = make_map(&q.mb, g.a, g.a_t, g.e.rows, g.inner, (uint32_t)q.bn)) != MP_OK) return s;
+  q.p.e = epi_of<bf16>(g.e);
+  q.p.kb = inner_stages(g);
+  q.p.tiles_r = (uint32_t)((g.e.rows + q.bn - 1) / q.bn);
+  q.tiles = q.p.tiles_r * ((g.e.cols + 127) / 128);
+  if (q.tiles > 0x7FFFFFFFull / 8) {
+    set_static_error("the output has too many tiles");
+    return MP_ERR_UNSUPPORTED;
+  }
+  return MP_OK;
+}
+
+// As many CTAs share a tile as keep at least two stages each while three to an SM hold them all, and they have as many
+// stages as shared memory holds then (with a tenth of the SMs' places to spare: clusters do not fill every one).
+// One row, 4096 -> 14336, 112 tiles: 26.8 us unsplit, 23.0 with two CTAs of 5 stages, 21.9 with four of 3, 29 with
+// four of 4 stages, which do not all fit; 24 rows, 14336 -> 4096, 32 tiles: 83 us unsplit, 25.1 with eight of 5.
+int split_stages(int bn, uint64_t ctas) {
+  const uint64_t sms = (uint64_t)device_sms();
+  const uint64_t per_sm = std::max<uint64_t>(1, std::min<uint64_t>(4, (ctas * 11 + sms * 10 - 1) / (sms * 10)));
+  return (int)std::min<uint64_t>(6, (228 * 1024 / per_sm - 2560) / (128 * 128 + bn * 128));
+}
+
 mp_status gemm_bf16(const GemmLaunch& g, cudaStream_t st) {
   mp_status s;
   if (large_product(g.e)) {
@@ -953,34 +1014,56 @@ mp_status gemm_bf16(const GemmLaunch& g, cudaStream_t st) {
            : g.b_t ? launch_large<false, true, false>(g, q, q, st)
                    : launch_large<false, false, false>(g, q, q, st);
   }
-  const Epi<bf16> e = epi_of<bf16>(g.e);
-  const uint32_t kb = inner_stages(g);
-  const uint64_t sms = (uint64_t)device_sms();
-  int bn = 128;  // rows of a tile
-  if (!g.a_t) bn = g.e.rows <= 16 ? 16 : g.e.rows <= 32 ? 32 : g.e.rows <= 64 ? 64 : 128;
-  CUtensorMap ma, mb;
-  if ((s = make_map(&ma, g.a, g.a_t, g.e.rows, g.inner, (uint32_t)bn)) != MP_OK) return s;
-  if ((s = make_map(&mb, g.b, g.b_t, g.e.cols, g.inner, 128u)) != MP_OK) return s;
-  const uint64_t tiles = ((g.e.rows + bn - 1) / bn) * ((g.e.cols + 127) / 128);
-  if (tiles > 0x7FFFFFFFull / 8) {
-    set_static_error("the output has too many tiles");
-    return MP_ERR_UNSUPPORTED;
-  }
-  // As many CTAs as share a tile while three to an SM hold them all and each has two stages at least, and as many
-  // stages as shared memory holds then (with a tenth of the SMs' places to spare: clusters do not fill every one).
-  // One row, 4096 -> 14336, 112 tiles: 26.8 us unsplit, 23.0 with two CTAs of 5 stages, 21.9 with four of 3, 29 with
-  // four of 4 stages, which do not all fit; 24 rows, 14336 -> 4096, 32 tiles: 83 us unsplit, 25.1 with eight of 5.
-  const int stage = 128 * 128 + bn * 128;
-  auto stages_with = [&](uint64_t ctas) {
-    const uint64_t per_sm = std::max<uint64_t>(1, std::min<uint64_t>(4, (ctas * 11 + sms * 10 - 1) / (sms * 10)));
-    return (int)std::min<uint64_t>(6, (228 * 1024 / per_sm - 2560) / stage);
-  };
+  SplitPlan q;
+  if ((s = prepare_split(g, q)) != MP_OK) return s;
   unsigned split = 1;
-  while (split < 8 && tiles * split * 2 <= sms * 3 && kb >= 4 * split && stages_with(tiles * split * 2) >= 2) split *= 2;
-  const int stages = std::max(2, stages_with(tiles * split));
-  const cudaError_t r = g.a_t   ? launch_split_of<true, true>(bn, mb, ma, e, kb, split, stages, g.wait, st)
-                        : g.b_t ? launch_split_of<true, false>(bn, mb, ma, e, kb, split, stages, g.wait, st)
-                                : launch_split_of<false, false>(bn, mb, ma, e, kb, split, stages, g.wait, st);
+  const uint64_t sms = (uint64_t)device_sms();
+  while (split < 8 && q.tiles * split * 2 <= sms * 3 && q.p.kb >= 4 * split && split_stages(q.bn, q.tiles * split * 2) >= 2)
+    split *= 2;
+  q.p.stages = (uint32_t)std::max(2, split_stages(q.bn, q.tiles * split));
+  auto go = [&](auto kernel) {
+    return launch_cluster(kernel, (unsigned)q.tiles * split, kGemmThreads, split, split_bytes(q.bn, (int)q.p.stages), st, q.ma,
+                          q.mb, q.p, g.wait);
+  };
+  cudaError_t r;
+  if (g.a_t)
+    r = go(split_kernel<128, true, true>);
+  else if (g.b_t)
+    r = q.bn == 16   ? go(split_kernel<16, true, false>)
+        : q.bn == 32 ? go(split_kernel<32, true, false>)
+        : q.bn == 64 ? go(split_kernel<64, true, false>)
+                     : go(split_kernel<128, true, false>);
+  else
+    r = q.bn == 16   ? go(split_kernel<16, false, false>)
+        : q.bn == 32 ? go(split_kernel<32, false, false>)
+        : q.bn == 64 ? go(split_kernel<64, false, false>)
+                     : go(split_kernel<128, false, false>);
+  return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
+}
+
+// dx and dw in one launch of clusters of one size, where three CTAs to an SM hold all tiles: such products wait for their
+// first bytes and for one another more than for anything else.  333 rows, 901 -> 1151: 13 and 14 us one after the
+// other.
+bool split_two(const SplitPlan& a, const SplitPlan& b) { return a.tiles + b.tiles <= 3ull * device_sms(); }
+
+mp_status launch_split_two(const GemmLaunch& g, SplitPlan& a, SplitPlan& b, cudaStream_t st) {
+  const uint64_t sms = (uint64_t)device_sms(), tiles = a.tiles + b.tiles;
+  const uint32_t kb = std::max(a.p.kb, b.p.kb);
+  unsigned split = 1;
+  while (split < 8 && tiles * split * 2 <= sms * 3 && kb >= 4 * split && split_stages(128, tiles * split * 2) >= 2) split *= 2;
+  const int stages = std::max(2, split_stages(128, tiles * split));
+  const size_t smem = split_bytes(128, stages);
+  b.p.stages = (uint32_t)stages;
+  a.p.stages = (uint32_t)std::min<size_t>(6, (smem - 1024) / (128 * 128 + a.bn * 128));
+  const unsigned blocks = (unsigned)a.tiles * split;
+  auto go = [&](auto kernel) {
+    return launch_cluster(kernel, (unsigned)tiles * split, kGemmThreads, split, smem, st, a.ma, a.mb, a.p, b.ma, b.mb, b.p, blocks,
+                          g.wait);
+  };
+  const cudaError_t r = a.bn == 16   ? go(split_two_kernel<16>)
+                        : a.bn == 32 ? go(split_two_kernel<32>)
+                        : a.bn == 64 ? go(split_two_kernel<64>)
+                                     : go(split_two_kernel<128>);
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
 
@@ -1037,8 +1120,21 @@ bool dz_vectors(const DzLaunch& p) {
 
 int dz_width(const DzLaunch& p) { return !dz_vectors(p) ? 1 : p.dtype == MP_BF16 ? 8 : 4; }
 
+// the kernels' arguments of n copies (two at most), and how many CTAs they are for
+template <typename T>
+uint64_t copy_args(const Copy* m, int n, CopyArgs<T>* a) {
+  uint64_t rows = 0;
+  for (int k = 0; k < 2; ++k) a[k] = CopyArgs<T>{};
+  for (int k = 0; k < n; ++k) {
+    a[k] = CopyArgs<T>{static_cast<const T*>(m[k].src.p), static_cast<T*>(m[k].dst), m[k].src.ld, m[k].ldd, m[k].rows,
+                       (uint32_t)m[k].cols};
+    rows = std::max(rows, m[k].rows);
+  }
+  return std::min<uint64_t>((rows + 7) / 8, 8ull * device_sms());
+}
+
 template <typename T, int V>
-cudaError_t dz_of(const DzLaunch& p, float* part, cudaStream_t st) {
+cudaError_t dz_of(const DzLaunch& p, const Copy* copies, int n, float* part, cudaStream_t st) {
   const DzPlan plan = dz_plan(p, V);
   DzArgs<T> a;
   a.rows = p.rows;
@@ -1059,20 +1155,30 @@ cudaError_t dz_of(const DzLaunch& p, float* part, cudaStream_t st) {
   a.lddmul = p.lddmul;
   a.db = static_cast<T*>(p.db);
   a.part = p.db && !plan.cluster ? part : nullptr;
-  const uint64_t ctas = plan.blocks * plan.parts;
+  const uint64_t blocks = plan.blocks * plan.parts;
+  a.blocks = (uint32_t)blocks;
+  uint64_t ctas = blocks + copy_args(copies, n, a.copy);
+  if (plan.cluster) ctas = (ctas + plan.parts - 1) / plan.parts * plan.parts;
   if (ctas > 0x7FFFFFFFull) return cudaErrorInvalidValue;
   auto go = [&](auto kernel) {
     return plan.cluster ? launch_cluster(kernel, (unsigned)ctas, 256, plan.parts, 0, st, a)
                         : launch_kernel(true, kernel, dim3((unsigned)ctas), 256, 0, st, a);
   };
+  auto with = [&](auto copy) {
+    constexpr bool C = decltype(copy)::value;
+    switch (p.act) {
+      case MP_ACT_RELU: return go(dz_kernel<T, V, MP_ACT_RELU, C>);
+      case MP_ACT_SILU: return go(dz_kernel<T, V, MP_ACT_SILU, C>);
+      case MP_ACT_GELU: return go(dz_kernel<T, V, MP_ACT_GELU, C>);
+      case MP_ACT_GELU_TANH: return go(dz_kernel<T, V, MP_ACT_GELU_TANH, C>);
+      default: return go(dz_kernel<T, V, MP_ACT_NONE, C>);
+    }
+  };
   cudaError_t e;
-  switch (p.act) {
-    case MP_ACT_RELU: e = go(dz_kernel<T, V, MP_ACT_RELU>); break;
-    case MP_ACT_SILU: e = go(dz_kernel<T, V, MP_ACT_SILU>); break;
-    case MP_ACT_GELU: e = go(dz_kernel<T, V, MP_ACT_GELU>); break;
-    case MP_ACT_GELU_TANH: e = go(dz_kernel<T, V, MP_ACT_GELU_TANH>); break;
-    default: e = go(dz_kernel<T, V, MP_ACT_NONE>); break;
-  }
+  if constexpr (sizeof(T) == 2)  // fp32 operands are read as they are
+    e = n ? with(std::true_type()) : with(std::false_type());
+  else
+    e = with(std::false_type());
   if (e != cudaSuccess || !a.part) return e;
   return launch_column_sums(p.dtype, part, plan.parts, (uint32_t)p.cols, p.db, st);
 }
@@ -1095,6 +1201,11 @@ mp_status launch_gemms(const GemmLaunch& dx, const GemmLaunch& dw, cudaStream_t 
     if ((s = prepare_large(dx, a)) != MP_OK || (s = prepare_large(dw, b)) != MP_OK) return s;
     return launch_large<false, true, true>(dx, a, b, st);
   }
+  if (dx.dtype == MP_BF16 && !large_product(dx.e) && !large_product(dw.e)) {
+    SplitPlan a, b;
+    if ((s = prepare_split(dx, a)) != MP_OK || (s = prepare_split(dw, b)) != MP_OK) return s;
+    if (split_two(a, b)) return launch_split_two(dx, a, b, st);
+  }
   if ((s = launch_gemm(dx, st)) != MP_OK) return s;
   return launch_gemm(dw, st);
 }
@@ -1105,23 +1216,17 @@ size_t dz_scratch(const DzLaunch& p) {
   return plan.cluster ? 0 : (size_t)plan.parts * p.cols * sizeof(float);
 }
 
-cudaError_t launch_dz(const DzLaunch& p, float* scratch, cudaStream_t st) {
+cudaError_t launch_dz(const DzLaunch& p, const Copy* copies, int n, float* scratch, cudaStream_t st) {
   const bool vec = dz_vectors(p);
-  if (p.dtype == MP_BF16) return vec ? dz_of<bf16, 8>(p, scratch, st) : dz_of<bf16, 1>(p, scratch, st);
-  return vec ? dz_of<float, 4>(p, scratch, st) : dz_of<float, 1>(p, scratch, st);
+  if (p.dtype == MP_BF16) return vec ? dz_of<bf16, 8>(p, copies, n, scratch, st) : dz_of<bf16, 1>(p, copies, n, scratch, st);
+  return vec ? dz_of<float, 4>(p, copies, n, scratch, st) : dz_of<float, 1>(p, copies, n, scratch, st);
 }
 
 template <typename T>
 cudaError_t copy_of(const Copy* m, int n, cudaStream_t st) {
-  CopyArgs<T> a[2] = {};
-  uint64_t rows = 0;
-  for (int k = 0; k < n; ++k) {
-    a[k] = CopyArgs<T>{static_cast<const T*>(m[k].src.p), static_cast<T*>(m[k].dst), m[k].src.ld, m[k].ldd, m[k].rows,
-                       (uint32_t)m[k].cols};
-    rows = std::max(rows, m[k].rows);
-  }
-  const dim3 grid((unsigned)std::min<uint64_t>((rows + 7) / 8, 8ull * device_sms()), n);
-  return launch_kernel(true, copy_kernel<T>, grid, 256, 0, st, a[0], a[1]);
+  CopyArgs<T> a[2];
+  const uint64_t ctas = copy_args(m, n, a);
+  return launch_kernel(true, copy_kernel<T>, dim3((unsigned)std::max<uint64_t>(1, ctas)), 256, 0, st, a[0], a[1]);
 }
 
 cudaError_t launch_copies(mp_dtype dtype, const Copy* m, int n, cudaStream_t st) {
