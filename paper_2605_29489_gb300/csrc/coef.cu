@@ -45,12 +45,16 @@ __device__ __forceinline__ uint4 load_vec(const T* p, uint32_t v, uint32_t n) {
   constexpr int V = Elem<T>::kVec;
   const uint32_t at = v * V;
   if (at + V <= n) return __ldcs(reinterpret_cast<const uint4*>(p + at));
-  Pack<T, V> q;
+  uint32_t w[4] = {};
 #pragma unroll
-  for (int e = 0; e < V; ++e) q.e[e] = at + e < n ? p[at + e] : T(0.0f);
-  uint4 u;
-  memcpy(&u, &q, 16);
-  return u;
+  for (int e = 0; e < V; ++e)
+    if (at + e < n) {
+      if constexpr (sizeof(T) == 2)
+        w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[at + e] << (16 * (e % 2));
+      else
+        w[e] = reinterpret_cast<const uint32_t*>(p)[at + e];
+    }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <typename T>

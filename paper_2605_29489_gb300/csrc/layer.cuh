@@ -74,64 +74,119 @@ struct Elem<__nv_bfloat16> {
   static __device__ __forceinline__ __nv_bfloat16 store(float v) { return __float2bfloat16_rn(v); }
 };
 
-// V consecutive elements as they are stored: one 16-byte register group, or a single element
+// V consecutive elements as they are stored: 32-bit words of them (8 or 16 bytes, accessed whole), or a single element.
+// Words, because elements of a struct are moved one by one: a bf16 row's elements then take three or four instructions
+// each to become fp32.
 template <typename T, int V>
 struct alignas(V * sizeof(T)) Pack {
-  T e[V];
+  uint32_t w[V * sizeof(T) / 4];
+};
+template <typename T>
+struct Pack<T, 1> {
+  T e;
 };
 template <typename T, int V>
 __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
   Pack<T, V> r;
   if constexpr (V * sizeof(T) == 16) {
     const uint4 u = *reinterpret_cast<const uint4*>(p);
-    memcpy(&r, &u, 16);
+    r.w[0] = u.x;
+    r.w[1] = u.y;
+    r.w[2] = u.z;
+    r.w[3] = u.w;
+  } else if constexpr (V * sizeof(T) == 8) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    r.w[0] = u.x;
+    r.w[1] = u.y;
   } else {
-    static_assert(V == 1, "whole vectors or single elements");
-    r.e[0] = *p;
+    static_assert(V == 1, "16 bytes, 8 bytes or one element");
+    r.e = *p;
   }
   return r;
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) {
-  if constexpr (V * sizeof(T) == 16) {
-    uint4 u;
-    memcpy(&u, &v, 16);
-    *reinterpret_cast<uint4*>(p) = u;
-  } else {
-    *p = v.e[0];
-  }
+  if constexpr (V * sizeof(T) == 16)
+    *reinterpret_cast<uint4*>(p) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+  else if constexpr (V * sizeof(T) == 8)
+    *reinterpret_cast<uint2*>(p) = make_uint2(v.w[0], v.w[1]);
+  else
+    *p = v.e;
 }
-
-// all elements of a pack at once as fp32, and back (rounded to nearest even): one instruction an element or less for
-// bf16, where taking them one by one costs three or four
+// all elements of a pack as fp32, and back (rounded to nearest even)
 template <typename T, int V>
 __device__ __forceinline__ void unpack(const Pack<T, V>& q, float* v) {
-  if constexpr (sizeof(T) == 2 && V % 2 == 0) {
-    uint32_t w[V / 2];
-    memcpy(w, &q, sizeof(w));
+  if constexpr (V == 1) {
+    v[0] = Elem<T>::load(q.e);
+  } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int k = 0; k < V / 2; ++k) {
-      v[2 * k] = __uint_as_float(w[k] << 16);
-      v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      v[2 * k] = __uint_as_float(q.w[k] << 16);
+      v[2 * k + 1] = __uint_as_float(q.w[k] & 0xFFFF0000u);
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = Elem<T>::load(q.e[k]);
+    for (int k = 0; k < V; ++k) v[k] = __uint_as_float(q.w[k]);
   }
 }
 template <typename T, int V>
 __device__ __forceinline__ Pack<T, V> pack(const float* v) {
   Pack<T, V> q;
-  if constexpr (sizeof(T) == 2 && V % 2 == 0) {
-    __nv_bfloat162 w[V / 2];
+  if constexpr (V == 1) {
+    q.e = Elem<T>::store(v[0]);
+  } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int k = 0; k < V / 2; ++k) w[k] = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-    memcpy(&q, w, sizeof(w));
+    for (int k = 0; k < V / 2; ++k)
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(q.w[k]) : "f"(v[2 * k + 1]), "f"(v[2 * k]));
   } else {
 #pragma unroll
-    for (int k = 0; k < V; ++k) q.e[k] = Elem<T>::store(v[k]);
+    for (int k = 0; k < V; ++k) q.w[k] = __float_as_uint(v[k]);
   }
   return q;
+}
+
+// two fp32 operations in one instruction, each rounded as on its own
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mul.rn.f32x2 rd, ra, rb;\n"
+      " mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n add.rn.f32x2 rd, ra, rb;\n"
+      " mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rc, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mov.b64 rc, {%6, %7};\n"
+      " fma.rn.f32x2 rd, ra, rb, rc;\n mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+// the elements of a pack as pairs
+template <typename T, int V>
+__device__ __forceinline__ void unpack2(const Pack<T, V>& q, float2* v) {
+  float f[V];
+  unpack(q, f);
+#pragma unroll
+  for (int k = 0; k < V / 2; ++k) v[k] = make_float2(f[2 * k], f[2 * k + 1]);
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> pack2(const float2* v) {
+  float f[V];
+#pragma unroll
+  for (int k = 0; k < V / 2; ++k) {
+    f[2 * k] = v[k].x;
+    f[2 * k + 1] = v[k].y;
+  }
+  return pack<T, V>(f);
 }
 
 // ---- norm.cu ------------------------------------------------------------------------------------

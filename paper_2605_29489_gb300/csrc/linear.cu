@@ -155,9 +155,9 @@ __device__ __forceinline__ void epi_quad(const Epi<T>& e, uint32_t r, uint32_t c
     return;
   }
   Pack<T, 4> m, s;
-  if (e.mul) m = *reinterpret_cast<const Pack<T, 4>*>(e.mul + r * e.ldmul + c);
-  if (e.res) s = *reinterpret_cast<const Pack<T, 4>*>(e.res + r * e.ldres + c);
-  if (e.pre) *reinterpret_cast<Pack<T, 4>*>(e.pre + r * e.ldpre + c) = pack<T, 4>(v);
+  if (e.mul) m = load_pack<T, 4>(e.mul + r * e.ldmul + c);
+  if (e.res) s = load_pack<T, 4>(e.res + r * e.ldres + c);
+  if (e.pre) store_pack<T, 4>(e.pre + r * e.ldpre + c, pack<T, 4>(v));
   act_all<FAST, 4>(e.act, v);
   float u[4];
   if (e.mul) {
@@ -170,7 +170,7 @@ __device__ __forceinline__ void epi_quad(const Epi<T>& e, uint32_t r, uint32_t c
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] += u[k];
   }
-  *reinterpret_cast<Pack<T, 4>*>(e.y + r * e.ldy + c) = pack<T, 4>(v);
+  store_pack<T, 4>(e.y + r * e.ldy + c, pack<T, 4>(v));
 }
 
 // N consecutive columns of a row, from c on (a multiple of N), of which those below e.cols exist

@@ -78,25 +78,34 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), kForward / cta_of<ROWT>()) nor
   const uint64_t step = (uint64_t)gridDim.x * kRows;
   constexpr bool kAhead = !(LAYER && V == 1 && sizeof(T) == 2);  // else the next row does not fit the registers
   auto place = [&](int k) { return (uint32_t)(k * ROWT + lane) * V; };
-  Pack<T, V> next[NV];
-  auto fetch = [&](uint64_t r) {
+  constexpr bool kAhead2 = V == 8;  // and the one after it, where both fit: with one, 32 KB an SM are on their way
+  Pack<T, V> next[NV], next2[NV];
+  auto fetch = [&](uint64_t r, Pack<T, V>* to) {
     const T* x = static_cast<const T*>(p.x) + r * p.ldx;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      if (place(k) < p.cols) next[k] = load_pack<T, V>(x + place(k));
+      if (place(k) < p.cols) to[k] = load_pack<T, V>(x + place(k));
   };
   uint64_t r0 = (uint64_t)blockIdx.x * kRows;
-  if (kAhead && r0 + threadIdx.x / ROWT < p.rows) fetch(r0 + threadIdx.x / ROWT);
+  if (kAhead && r0 + threadIdx.x / ROWT < p.rows) fetch(r0 + threadIdx.x / ROWT, next);
+  if (kAhead2 && r0 + step + threadIdx.x / ROWT < p.rows) fetch(r0 + step + threadIdx.x / ROWT, next2);
   // the rows of a CTA go on together (its threads meet at the sums): r0 is the same for all of them
   for (; r0 < p.rows; r0 += step) {
     const uint64_t r = r0 + threadIdx.x / ROWT;
     Pack<T, V> q[NV];
     float v[V];
     float s = 0.0f;
-    if (!kAhead && r < p.rows) fetch(r);
+    if (!kAhead && r < p.rows) fetch(r, next);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) q[k] = next[k];
-    if (kAhead && r + step < p.rows) fetch(r + step);
+    for (int k = 0; k < NV; ++k) {
+      q[k] = next[k];
+      if (kAhead2) next[k] = next2[k];
+    }
+    if (kAhead2) {
+      if (r + 2 * step < p.rows) fetch(r + 2 * step, next2);
+    } else if (kAhead && r + step < p.rows) {
+      fetch(r + step, next);
+    }
 #pragma unroll
     for (int k = 0; k < NV; ++k)
       if (place(k) < p.cols) {
@@ -161,20 +170,19 @@ __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) 
     float mu = 0.0f, s = 0.0f;
     if (LAYER) {
       for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
-        const Pack<T, V> q = load_pack<T, V>(x + c);
+        float v[V];
+        unpack(load_pack<T, V>(x + c), v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) s += Elem<T>::load(q.e[e]);
+        for (int e = 0; e < V; ++e) s += v[e];
       }
       mu = row_sum<1024, false>(s, 0.0f, red, turn).x * inv;
       s = 0.0f;
     }
     for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
-      const Pack<T, V> q = load_pack<T, V>(x + c);
+      float v[V];
+      unpack(load_pack<T, V>(x + c), v);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float t = Elem<T>::load(q.e[e]) - mu;
-        s = fmaf(t, t, s);
-      }
+      for (int e = 0; e < V; ++e) s = fmaf(v[e] - mu, v[e] - mu, s);
     }
     const float rstd = 1.0f / sqrtf(row_sum<1024, false>(s, 0.0f, red, turn).x * inv + p.eps);
     if (threadIdx.x == 0) {
@@ -183,18 +191,21 @@ __global__ void __launch_bounds__(1024, 1) norm_wide_kernel(const NormLaunch p) 
     }
     T* y = static_cast<T*>(p.y) + r * p.ldy;
     for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
-      const Pack<T, V> q = load_pack<T, V>(x + c);
-      Pack<T, V> o, wq, bq;
-      if (w) wq = load_pack<T, V>(w + c);
-      if (b) bq = load_pack<T, V>(b + c);
+      float v[V], u[V];
+      unpack(load_pack<T, V>(x + c), v);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        float t = (Elem<T>::load(q.e[e]) - mu) * rstd;
-        if (w) t *= Elem<T>::load(wq.e[e]);
-        if (b) t += Elem<T>::load(bq.e[e]);
-        o.e[e] = Elem<T>::store(t);
+      for (int e = 0; e < V; ++e) v[e] = (v[e] - mu) * rstd;
+      if (w) {
+        unpack(load_pack<T, V>(w + c), u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] *= u[e];
       }
-      store_pack<T, V>(y + c, o);
+      if (b) {
+        unpack(load_pack<T, V>(b + c), u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += u[e];
+      }
+      store_pack<T, V>(y + c, pack<T, V>(v));
     }
   }
 }
@@ -358,7 +369,8 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_backward_ring_kernel(con
   }
   __syncthreads();
   const uint64_t n_rows = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // of this CTA: blockIdx.x + n gridDim.x
-  float aw[16] = {}, ab[16] = {};
+  constexpr int P = V / 2;  // pairs of a vector
+  float2 aw[8] = {}, ab[8] = {};
   const uint32_t group = warp / kGroupWarps, at = threadIdx.x % ROWT;
   if (warp == 16) {
     uint64_t n = 0;
@@ -405,34 +417,36 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_backward_ring_kernel(con
       const T* x = reinterpret_cast<const T*>(ring + s * slot_bytes);
       const T* dy = reinterpret_cast<const T*>(ring + s * slot_bytes + row_bytes);
       const T* add = reinterpret_cast<const T*>(ring + s * slot_bytes + 2 * row_bytes);
-      float h[16], g[16], u[V];
-      float s1 = 0.0f, s2 = 0.0f;
+      float2 h[8], g[8], u[P];
+      float2 t1 = {0.0f, 0.0f}, t2 = {0.0f, 0.0f};
       Pack<T, V> aq[NV];
-      // 16 columns' xh in hk and dy in gk; then the weight in u
-      auto take = [&](int k, float* hk, float* gk) {
-        unpack(load_pack<T, V>(x + place(k)), hk);
-        unpack(load_pack<T, V>(dy + place(k)), gk);
-        if (w) unpack(load_pack<T, V>(w + place(k)), u);
+      const float2 scale = {rstd, rstd}, shift = {-mu, -mu};
+      // V columns' xh in hk and dy in gk; then the weight in u
+      auto take = [&](int k, float2* hk, float2* gk) {
+        unpack2(load_pack<T, V>(x + place(k)), hk);
+        unpack2(load_pack<T, V>(dy + place(k)), gk);
+        if (w) unpack2(load_pack<T, V>(w + place(k)), u);
 #pragma unroll
-        for (int e = 0; e < V; ++e) hk[e] = (LAYER ? hk[e] - mu : hk[e]) * rstd;
+        for (int e = 0; e < P; ++e) hk[e] = mul2(LAYER ? add2(hk[e], shift) : hk[e], scale);
       };
 #pragma unroll
       for (int k = 0; k < NV; ++k)
         if (place(k) < p.cols) {
-          float *hk = h + k * V, *gk = g + k * V;
+          float2 *hk = h + k * P, *gk = g + k * P;
           take(k, hk, gk);
           if (kKeep && p.add) aq[k] = load_pack<T, V>(add + place(k));
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            aw[k * V + e] = fmaf(gk[e], hk[e], aw[k * V + e]);
-            if (LAYER) ab[k * V + e] += gk[e];
-            if (w) gk[e] *= u[e];
-            s1 = fmaf(gk[e], hk[e], s1);
-            if (LAYER) s2 += gk[e];
+          for (int e = 0; e < P; ++e) {
+            aw[k * P + e] = fma2(gk[e], hk[e], aw[k * P + e]);
+            if (LAYER) ab[k * P + e] = add2(ab[k * P + e], gk[e]);
+            if (w) gk[e] = mul2(gk[e], u[e]);
+            t1 = fma2(gk[e], hk[e], t1);
+            if (LAYER) t2 = add2(t2, gk[e]);
           }
         }
       __syncwarp();
       if ((kKeep || !p.dx) && lane == 0) mbar_arrive(&empty[s]);
+      float s1 = t1.x + t1.y, s2 = t2.x + t2.y;
       if (!p.dx) continue;
       s1 = warp_sum(s1);
       if (LAYER) s2 = warp_sum(s2);
@@ -450,25 +464,25 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_backward_ring_kernel(con
         s1 += __shfl_xor_sync(0xFFFFFFFFu, s1, o);
         if (LAYER) s2 += __shfl_xor_sync(0xFFFFFFFFu, s2, o);
       }
-      const float m1 = s1 * inv, m2 = s2 * inv;
+      const float2 m1 = {-s1 * inv, -s1 * inv}, m2 = {-s2 * inv, -s2 * inv};
       T* dx = static_cast<T*>(p.dx) + (blockIdx.x + n * gridDim.x) * p.lddx;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
         if (place(k) < p.cols) {
-          float *hk = h + k * V, *gk = g + k * V;
+          float2 *hk = h + k * P, *gk = g + k * P;
           if (!kKeep) {
             take(k, hk, gk);
             if (w)
 #pragma unroll
-              for (int e = 0; e < V; ++e) gk[e] *= u[e];
+              for (int e = 0; e < P; ++e) gk[e] = mul2(gk[e], u[e]);
           }
-          if (p.add) unpack(kKeep ? aq[k] : load_pack<T, V>(add + place(k)), u);
+          if (p.add) unpack2(kKeep ? aq[k] : load_pack<T, V>(add + place(k)), u);
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            gk[e] = fmaf(-hk[e], m1, LAYER ? gk[e] - m2 : gk[e]) * rstd;
-            if (p.add) gk[e] += u[e];
+          for (int e = 0; e < P; ++e) {
+            gk[e] = mul2(fma2(hk[e], m1, LAYER ? add2(gk[e], m2) : gk[e]), scale);
+            if (p.add) gk[e] = add2(gk[e], u[e]);
           }
-          store_pack<T, V>(dx + place(k), pack<T, V>(gk));
+          store_pack<T, V>(dx + place(k), pack2<T, V>(gk));
         }
       __syncwarp();
       if (!kKeep && lane == 0) mbar_arrive(&empty[s]);
@@ -485,7 +499,8 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_backward_ring_kernel(con
         const uint32_t c = (uint32_t)(k * ROWT + at) * V;
         if (c < p.cols)
 #pragma unroll
-          for (int e = 0; e < V; ++e) sums[group * p.cols + c + e] = which ? ab[k * V + e] : aw[k * V + e];
+          for (int e = 0; e < P; ++e)
+            *reinterpret_cast<float2*>(sums + group * p.cols + c + 2 * e) = which ? ab[k * P + e] : aw[k * P + e];
       }
     }
     __syncthreads();
@@ -514,35 +529,36 @@ __global__ void __launch_bounds__(1024, 1) norm_backward_wide_kernel(const NormL
     const float mu = LAYER ? p.mean[r] : 0.0f, rstd = p.rstd[r];
     float s1 = 0.0f, s2 = 0.0f;
     for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
-      const Pack<T, V> xq = load_pack<T, V>(x + c), dq = load_pack<T, V>(dy + c);
-      Pack<T, V> wq;
-      if (w) wq = load_pack<T, V>(w + c);
+      float h[V], g[V], u[V];
+      unpack(load_pack<T, V>(x + c), h);
+      unpack(load_pack<T, V>(dy + c), g);
+      if (w) unpack(load_pack<T, V>(w + c), u);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float d = Elem<T>::load(dq.e[e]);
-        const float g = w ? d * Elem<T>::load(wq.e[e]) : d;
-        s1 = fmaf(g, (Elem<T>::load(xq.e[e]) - mu) * rstd, s1);
-        s2 += g;
+        if (w) g[e] *= u[e];
+        s1 = fmaf(g[e], (h[e] - mu) * rstd, s1);
+        s2 += g[e];
       }
     }
     const float2 m = row_sum<1024, true>(s1, s2, red, turn);
     const float m1 = m.x * inv, m2 = LAYER ? m.y * inv : 0.0f;
     T* dx = static_cast<T*>(p.dx) + r * p.lddx;
     for (uint32_t c = threadIdx.x * V; c < p.cols; c += 1024u * V) {
-      const Pack<T, V> xq = load_pack<T, V>(x + c), dq = load_pack<T, V>(dy + c);
-      Pack<T, V> wq, aq, o;
-      if (w) wq = load_pack<T, V>(w + c);
-      if (add) aq = load_pack<T, V>(add + c);
+      float h[V], g[V], u[V];
+      unpack(load_pack<T, V>(x + c), h);
+      unpack(load_pack<T, V>(dy + c), g);
+      if (w) {
+        unpack(load_pack<T, V>(w + c), u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[e] *= u[e];
+      }
+      if (add) unpack(load_pack<T, V>(add + c), u);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float d = Elem<T>::load(dq.e[e]);
-        const float g = w ? d * Elem<T>::load(wq.e[e]) : d;
-        const float h = (Elem<T>::load(xq.e[e]) - mu) * rstd;
-        float t = (g - m2 - h * m1) * rstd;
-        if (add) t += Elem<T>::load(aq.e[e]);
-        o.e[e] = Elem<T>::store(t);
+        g[e] = fmaf(-(h[e] - mu) * rstd, m1, g[e] - m2) * rstd;
+        if (add) g[e] += u[e];
       }
-      store_pack<T, V>(dx + c, o);
+      store_pack<T, V>(dx + c, pack<T, V>(g));
     }
   }
 }
