@@ -102,7 +102,7 @@ def near(got, want, bound, what):
 NORM_SHAPES = [(1, 1), (1, 896), (3, 8), (5, 7), (2, 33), (9, 257), (130, 128), (64, 1024), (33, 2056), (700, 1537),
                (17, 4096), (3, 5003), (5, 8192), (2, 8200), (3, 12288), (2, 16384), (2, 16400), (1, 20001), (1201, 64),
                # many rows of whole vectors: the backward pass's ring, of every width and number of slots
-               (700, 1024), (1300, 1032), (611, 2056), (777, 4096), (640, 8192)]
+               (700, 1024), (1300, 1032), (611, 2056), (777, 4096), (640, 8192), (3001, 256), (900, 512), (1000, 520), (2000, 896)]
 
 
 @pytest.mark.parametrize("shape", NORM_SHAPES)
