@@ -1499,23 +1499,8 @@ mp_status merge_common(const mp_family* family, const mp_index* index, const mp_
   return MP_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-mp_status mp_merge(const mp_family* family, const mp_index* index, const mp_plan_t* plan, void* out_buf,
-                   mp_stream stream, mp_manifest** man_out) {
-  return merge_common(family, index, plan, out_buf, stream, man_out, false);
-}
-
-mp_status mp_merge_touched(const mp_family* family, const mp_index* index, const mp_plan_t* plan, void* out_buf,
-                           mp_stream stream, mp_manifest** man_out) {
-  return merge_common(family, index, plan, out_buf, stream, man_out, true);
-}
-
-mp_status mp_coef_grad(const mp_family* family, const mp_index* index, const mp_plan_t* plan, const void* grad,
-                       float* out, mp_stream stream) {
-  NvtxScope nv("mp_coef_grad");
+mp_status coef_grad(const mp_family* family, const mp_index* index, const mp_plan_t* plan, const void* grad, float* out,
+                    mp_stream stream) {
   mp_status st;
   if ((st = check_handle(index, kMagicIndex, "index")) != MP_OK) return st;
   if ((st = check_handle(plan, kMagicPlan, "plan")) != MP_OK) return st;
@@ -1564,6 +1549,7 @@ mp_status mp_coef_grad(const mp_family* family, const mp_index* index, const mp_
   p.mask = plan->d_mask;
   p.out = out;
   p.ext = Extents{g.span_elems, g.span_elems};
+  if (!(p.err = layer_error_word())) return fail(MP_ERR_OOM, "pinned host allocation failed");
   Event done;  // made before the launch, so that what is enqueued has an end to wait for
   if (!now_captured && (e = done.make()) != cudaSuccess) return cuda_fail(e, "event");
   Scratch s;
@@ -1576,14 +1562,49 @@ mp_status mp_coef_grad(const mp_family* family, const mp_index* index, const mp_
   return MP_OK;
 }
 
-mp_status mp_layer_status(mp_stream stream) {
+mp_status layer_status(mp_stream stream) {
   const cudaError_t e = cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "stream");
   uint32_t* w = layer_error_word();
   const uint32_t err = w ? __atomic_exchange_n(w, 0u, __ATOMIC_ACQ_REL) : 0u;
   if (err & kErrTimeout) return fail(MP_ERR_TIMEOUT, "a bounded device wait in a layer operator gave up");
+  if (err & kErrBounds) return fail(MP_ERR_CUDA, "a bounds check of the checked build failed in the layer kernels");
   if (err) return fail(MP_ERR_CUDA, "an internal check of the layer kernels failed");
   return MP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+mp_status mp_merge(const mp_family* family, const mp_index* index, const mp_plan_t* plan, void* out_buf,
+                   mp_stream stream, mp_manifest** man_out) {
+  return merge_common(family, index, plan, out_buf, stream, man_out, false);
+}
+
+mp_status mp_merge_touched(const mp_family* family, const mp_index* index, const mp_plan_t* plan, void* out_buf,
+                           mp_stream stream, mp_manifest** man_out) {
+  return merge_common(family, index, plan, out_buf, stream, man_out, true);
+}
+
+mp_status mp_coef_grad(const mp_family* family, const mp_index* index, const mp_plan_t* plan, const void* grad,
+                       float* out, mp_stream stream) {
+  NvtxScope nv("mp_coef_grad");
+  try {
+    return coef_grad(family, index, plan, grad, out, stream);
+  } catch (...) {
+    set_static_error("host allocation failed");
+    return MP_ERR_OOM;
+  }
+}
+
+mp_status mp_layer_status(mp_stream stream) {
+  try {
+    return layer_status(stream);
+  } catch (...) {
+    set_static_error("host allocation failed");
+    return MP_ERR_OOM;
+  }
 }
 
 mp_status mp_trim(void) {

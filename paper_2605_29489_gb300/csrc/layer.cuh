@@ -225,6 +225,7 @@ struct CoefLaunch {
   const uint32_t* mask;
   float* out;  // [K][n_tensors]
   Extents ext;
+  uint32_t* err;  // the host's error word (checked build)
 };
 size_t coef_scratch(const CoefLaunch& p);
 cudaError_t launch_coef(const CoefLaunch& p, float* scratch, cudaStream_t st);

@@ -17,7 +17,7 @@
 //                 and all SMs have to stream them, and for products too small to fill the GPU with tiles of 256.
 //
 // fp32 operands are multiplied in fp32 (fma) by a tiled kernel of the ordinary cores: a checkpoint kept
-// in fp32 is kept so for its accuracy, and splitting into tensor-core types does not hold it over long sums.
+// in fp32 is kept so for its accuracy, which sums of fp32 fma hold at every length.
 #include <dlfcn.h>
 
 #include <algorithm>
@@ -615,87 +615,137 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
 
 // ---- fp32 products --------------------------------------------------------------------------------
 
-// out[r, c] = sum over k of a(r, k) b(c, k), element (r, k) at a + r * ar + k * ak: tiles of 64 R x 64 R, BK k at a time,
-// 4 R x 4 R sums a thread.  The next step's elements are on their way while this one's are multiplied.  With R = 1 the
-// inner dimension may be split over a cluster, whose sums are added over distributed shared memory in the CTAs'
-// order: a product of 512 x 512 x 512 is a chain of steps of about 1 us on 64 CTAs, a quarter of it on 256.
-template <int R, int BK>
-__global__ void __launch_bounds__(256, R == 1 ? 2 : 1) gemm_f32_kernel(const float* a, uint64_t ar, uint64_t ak, const float* b, uint64_t br,
-                                                       uint64_t bk, uint32_t inner, uint32_t k_each, const Epi<float> e) {
+// An operand of an fp32 product: element (r, k) at p + r * sr + k * sk, one of the strides being 1; vec: rows of whole
+// 16-byte vectors along that one
+struct F32Operand {
+  const float* p;
+  uint64_t sr, sk;
+  uint32_t rows, vec;
+};
+
+// out[r, c] = sum over k of a(r, k) b(c, k), in fp32 fma: a thread has RG x CG blocks of 4 x 4 sums, a CTA of T threads a tile of
+// T / 4 * RG rows and 64 CG columns, BK k at a time.  The next step's elements are on their way while this one's are multiplied, two
+// sums to an instruction.  A tile lies in shared memory k by k, its rows in groups of four, group g of step k at place
+// g ^ (k / 4 mod 8): stores of 8 x 4 k by 4 rows, as a warp loads them along k, and loads of four rows each come to different banks.
+// The inner dimension may be split over a cluster, whose sums are added over distributed shared memory in the CTAs'
+// order.  Bound by the fma pipes where tiles fill the SMs, else by the steps' latency: 1024 x 1024 x 1024, 256 tiles of 64 x 64
+// split in two, 60 us (36 TFLOP/s); with 4 x 4 sums a thread, unsplit and element by element it was 86.
+template <int RG, int CG, int BK, int T>
+__global__ void __launch_bounds__(T, T == 128 ? 4 : 1) gemm_f32_kernel(const F32Operand a, const F32Operand b, uint32_t inner,
+                                                                       uint32_t k_each, const Epi<float> e) {
   kernel_begin();
-  constexpr uint32_t kTile = 64 * R, kPitch = kTile + 4;
-  constexpr int kLoads = kTile * BK / 256;
-  __shared__ alignas(16) float stage[2][2][BK][kPitch];  // [turn][operand]
-  const uint32_t rank = R == 1 ? cluster_rank() : 0u;
-  uint32_t split = 1;
-  if (R == 1) asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(split));
-  const uint32_t tiles_c = (e.cols + kTile - 1) / kTile, tile = blockIdx.x / split;
-  const uint32_t r0 = tile / tiles_c * kTile, c0 = tile % tiles_c * kTile;
-  const uint32_t first = rank * k_each, last = min(inner, first + k_each);
+  constexpr uint32_t kTR = T / 16 * 4 * RG, kTC = 64 * CG;  // rows and columns of a tile
+  constexpr int kLa = kTR * BK / 4 / T, kLb = kTC * BK / 4 / T;
+  __shared__ alignas(16) float sa[2][BK * kTR], sb[2][BK * kTC];
+  uint32_t split;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(split));
+  const uint32_t rank = cluster_rank();
+  const uint32_t tiles_c = (e.cols + kTC - 1) / kTC, tile = blockIdx.x / split;
+  const uint32_t r0 = tile / tiles_c * kTR, c0 = tile % tiles_c * kTC;
+  const uint32_t first = min(inner, rank * k_each), last = min(inner, first + k_each);
   const uint32_t t = threadIdx.x, tr = t / 16u, tc = t % 16u;
-  // element q of this thread's share of a tile: along k first where k is contiguous, else along the rows
-  auto spot = [&](uint64_t sk, int q, uint32_t& row, uint32_t& k) {
-    if (sk == 1) {
-      k = t % BK;
-      row = t / BK + (256u / BK) * q;
-    } else {
-      row = t % kTile;
-      k = t / kTile + (256u / kTile) * q;
-    }
-  };
-  float ra[kLoads], rb[kLoads];
-  auto fetch = [&](uint32_t k0) {
+  auto fetch = [&](auto rows_of, const F32Operand& o, uint32_t at, uint32_t k0, float4* to) {
+    constexpr uint32_t kRows = decltype(rows_of)::value;
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q) {
-      uint32_t row, k;
-      spot(ak, q, row, k);
-      ra[q] = r0 + row < e.rows && k0 + k < last ? a[(r0 + row) * ar + (k0 + k) * ak] : 0.0f;
-      spot(bk, q, row, k);
-      rb[q] = c0 + row < e.cols && k0 + k < last ? b[(c0 + row) * br + (k0 + k) * bk] : 0.0f;
-    }
-  };
-  auto put = [&](int s) {
+    for (int q = 0; q < (int)(kRows * BK / 4 / T); ++q) {
+      const uint32_t i = t + T * q;
+      float v[4] = {};
+      if (o.sk == 1) {
+        const uint32_t row = at + i / (BK / 4), k = k0 + i % (BK / 4) * 4;
+        const float* src = o.p + row * o.sr + k;
+        if (row < o.rows) {
+          if (o.vec && k + 4 <= last) {
+            *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
+          } else {
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q) {
-      uint32_t row, k;
-      spot(ak, q, row, k);
-      stage[s][0][k][row] = ra[q];
-      spot(bk, q, row, k);
-      stage[s][1][k][row] = rb[q];
+            for (int j = 0; j < 4; ++j)
+              if (k + j < last) v[j] = src[j];
+          }
+        }
+      } else {
+        const uint32_t row = at + i % (kRows / 4) * 4, k = k0 + i / (kRows / 4);
+        const float* src = o.p + k * o.sk + row;
+        if (k < last) {
+          if (o.vec && row + 4 <= o.rows) {
+            *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (row + j < o.rows) v[j] = src[j];
+          }
+        }
+      }
+      to[q] = make_float4(v[0], v[1], v[2], v[3]);
     }
   };
-  float acc[4 * R][4 * R] = {};
-  fetch(first);
-  put(0);
+  auto put = [&](auto rows_of, uint64_t sk, const float4* from, float* to) {
+    constexpr uint32_t kRows = decltype(rows_of)::value;
+#pragma unroll
+    for (int q = 0; q < (int)(kRows * BK / 4 / T); ++q) {
+      const uint32_t i = t + T * q;
+      if (sk == 1) {
+        const uint32_t row = i / (BK / 4), k4 = i % (BK / 4);
+        float* dst = to + k4 * 4 * kRows + ((row / 4) ^ (k4 % 8)) * 4 + row % 4;
+        dst[0] = from[q].x;
+        dst[kRows] = from[q].y;
+        dst[2 * kRows] = from[q].z;
+        dst[3 * kRows] = from[q].w;
+      } else {
+        const uint32_t g = i % (kRows / 4), k = i / (kRows / 4);
+        *reinterpret_cast<float4*>(to + k * kRows + (g ^ (k / 4 % 8)) * 4) = from[q];
+      }
+    }
+  };
+  using RowsA = std::integral_constant<uint32_t, kTR>;
+  using RowsB = std::integral_constant<uint32_t, kTC>;
+  float4 la[kLa], lb[kLb];
+  float2 acc[4 * RG][2 * CG] = {};
+  fetch(RowsA(), a, r0, first, la);
+  fetch(RowsB(), b, c0, first, lb);
+  put(RowsA(), a.sk, la, sa[0]);
+  put(RowsB(), b.sk, lb, sb[0]);
   __syncthreads();
   int s = 0;
   for (uint32_t k0 = first; k0 < last; k0 += BK, s ^= 1) {
     const bool more = k0 + BK < last;
-    if (more) fetch(k0 + BK);
+    if (more) {
+      fetch(RowsA(), a, r0, k0 + BK, la);
+      fetch(RowsB(), b, c0, k0 + BK, lb);
+    }
 #pragma unroll
     for (int k = 0; k < BK; ++k) {
-      float x[4 * R], y[4 * R];
+      float4 x[RG], y[CG];
 #pragma unroll
-      for (int h = 0; h < R; ++h) {
-        *reinterpret_cast<float4*>(x + 4 * h) = *reinterpret_cast<const float4*>(&stage[s][0][k][h * 64 + tr * 4u]);
-        *reinterpret_cast<float4*>(y + 4 * h) = *reinterpret_cast<const float4*>(&stage[s][1][k][h * 64 + tc * 4u]);
+      for (int h = 0; h < RG; ++h)
+        x[h] = *reinterpret_cast<const float4*>(&sa[s][k * kTR + ((tr + h * (T / 16)) ^ (k / 4 % 8)) * 4]);
+#pragma unroll
+      for (int h = 0; h < CG; ++h) y[h] = *reinterpret_cast<const float4*>(&sb[s][k * kTC + ((tc + h * 16) ^ (k / 4 % 8)) * 4]);
+#pragma unroll
+      for (int i = 0; i < 4 * RG; ++i) {
+        const float xi = i % 4 == 0 ? x[i / 4].x : i % 4 == 1 ? x[i / 4].y : i % 4 == 2 ? x[i / 4].z : x[i / 4].w;
+#pragma unroll
+        for (int h = 0; h < CG; ++h) {
+          acc[i][2 * h] = fma2(make_float2(xi, xi), make_float2(y[h].x, y[h].y), acc[i][2 * h]);
+          acc[i][2 * h + 1] = fma2(make_float2(xi, xi), make_float2(y[h].z, y[h].w), acc[i][2 * h + 1]);
+        }
       }
-#pragma unroll
-      for (int i = 0; i < 4 * R; ++i)
-#pragma unroll
-        for (int j = 0; j < 4 * R; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
     }
-    if (more) put(s ^ 1);
+    if (more) {
+      put(RowsA(), a.sk, la, sa[s ^ 1]);
+      put(RowsB(), b.sk, lb, sb[s ^ 1]);
+    }
     __syncthreads();
   }
-  if constexpr (R == 1) {
+  if constexpr (T == 128) {
     if (split > 1) {
-      float* sum = &stage[0][0][0][0];  // [64][64]
-      static_assert(sizeof(stage) >= 64 * 64 * 4, "the sums fit the stages");
+      float* sum = &sa[0][0];  // [kTR][64]
+      static_assert(sizeof(sa) >= kTR * 64 * 4, "the sums fit the stages");
 #pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(sum + (tr * 4u + i) * 64u + tc * 4u) = *reinterpret_cast<float4*>(acc[i]);
+      for (int i = 0; i < 4 * RG; ++i)
+        *reinterpret_cast<float4*>(sum + ((tr + i / 4 * (T / 16)) * 4 + i % 4) * 64 + tc * 4) =
+            make_float4(acc[i][0].x, acc[i][0].y, acc[i][1].x, acc[i][1].y);
       cluster_sync();
-      for (uint32_t r = 64u * rank / split + tr; r < 64u * (rank + 1) / split; r += 16u) {
+      for (uint32_t r = kTR * rank / split + tr; r < kTR * (rank + 1) / split; r += T / 16) {
         float v[4] = {};
         const uint32_t at = su32(sum + r * 64u + tc * 4u);
         for (uint32_t q = 0; q < split; ++q) {
@@ -712,10 +762,12 @@ __global__ void __launch_bounds__(256, R == 1 ? 2 : 1) gemm_f32_kernel(const flo
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4 * R; ++i)
+  for (int i = 0; i < 4 * RG; ++i)
 #pragma unroll
-    for (int h = 0; h < R; ++h)
-      epi_run<float, 4>(e, r0 + (i / 4) * 64u + tr * 4u + i % 4, c0 + h * 64u + tc * 4u, acc[i] + 4 * h);
+    for (int h = 0; h < CG; ++h) {
+      float v[4] = {acc[i][2 * h].x, acc[i][2 * h].y, acc[i][2 * h + 1].x, acc[i][2 * h + 1].y};
+      epi_run<float, 4>(e, r0 + (tr + i / 4 * (T / 16)) * 4u + i % 4, c0 + h * 64u + tc * 4u, v);
+    }
 }
 
 // ---- elementwise and layout kernels ---------------------------------------------------------------
@@ -946,6 +998,13 @@ bool large_product(const Epilogue& e) {
 
 uint32_t inner_stages(const GemmLaunch& g) { return (uint32_t)((g.inner + kBK - 1) / kBK); }
 
+// The bounded waits cover the longest there is, for all products of a tile: more rounds for long inner dimensions.
+Wait wait_of(const GemmLaunch& g, uint32_t kb) {
+  Wait w = g.wait;
+  if (!w.stall) w.limit = (uint32_t)std::min<uint64_t>(0xFFFFFFFFu, w.limit + 64ull * kb);
+  return w;
+}
+
 mp_status prepare_large(const GemmLaunch& g, Prepared& q) {
   mp_status s;
   if ((s = make_map(&q.ma, g.a, g.a_t, g.e.rows, g.inner, 128u)) != MP_OK) return s;
@@ -967,7 +1026,7 @@ mp_status launch_large(const GemmLaunch& g, const Prepared& a, const Prepared& b
   const uint64_t tiles = (uint64_t)a.p.tiles_r * a.p.tiles_c + (TWO ? (uint64_t)b.p.tiles_r * b.p.tiles_c : 0u);
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)device_sms() / 2);
   const cudaError_t r = launch_cluster(gemm_kernel<AT, BT, TWO>, pairs * 2, kGemmThreads, 2, 6 * 32768 + 1024, st, a.ma, a.mb,
-                                       a.p, b.ma, b.mb, b.p, g.wait);
+                                       a.p, b.ma, b.mb, b.p, wait_of(g, std::max(a.p.kb, b.p.kb)));
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
 
@@ -1023,7 +1082,7 @@ mp_status gemm_bf16(const GemmLaunch& g, cudaStream_t st) {
   q.p.stages = (uint32_t)std::max(2, split_stages(q.bn, q.tiles * split));
   auto go = [&](auto kernel) {
     return launch_cluster(kernel, (unsigned)q.tiles * split, kGemmThreads, split, split_bytes(q.bn, (int)q.p.stages), st, q.ma,
-                          q.mb, q.p, g.wait);
+                          q.mb, q.p, wait_of(g, q.p.kb));
   };
   cudaError_t r;
   if (g.a_t)
@@ -1058,7 +1117,7 @@ mp_status launch_split_two(const GemmLaunch& g, SplitPlan& a, SplitPlan& b, cuda
   const unsigned blocks = (unsigned)a.tiles * split;
   auto go = [&](auto kernel) {
     return launch_cluster(kernel, (unsigned)tiles * split, kGemmThreads, split, smem, st, a.ma, a.mb, a.p, b.ma, b.mb, b.p, blocks,
-                          g.wait);
+                          wait_of(g, kb));
   };
   const cudaError_t r = a.bn == 16   ? go(split_two_kernel<16>)
                         : a.bn == 32 ? go(split_two_kernel<32>)
@@ -1070,21 +1129,26 @@ mp_status launch_split_two(const GemmLaunch& g, SplitPlan& a, SplitPlan& b, cuda
 mp_status gemm_f32(const GemmLaunch& g, cudaStream_t st) {
   const Epi<float> e = epi_of<float>(g.e);
   auto tiles_of = [&](uint64_t n) { return ((g.e.rows + n - 1) / n) * ((g.e.cols + n - 1) / n); };
-  const uint64_t sms = (uint64_t)device_sms(), one = 1;
-  const bool large = tiles_of(128) >= sms;  // tiles of 128 fill the GPU
+  const uint64_t sms = (uint64_t)device_sms();
+  // tiles of 128 x 128, which read shared memory half as often, where there are two for each SM at least; below, tiles of
+  // 64 x 64 and as many CTAs to a tile as four to an SM hold (512 x 512 x 512: 32 us unsplit, 15 with four)
+  const bool large = tiles_of(128) >= 2 * sms;
   const uint64_t tiles = tiles_of(large ? 128 : 64);
-  if (tiles > 0x7FFFFFFFull) {
+  if (tiles > 0x7FFFFFFFull / 8) {
     set_static_error("the output has too many tiles");
     return MP_ERR_UNSUPPORTED;
   }
   unsigned split = 1;
-  while (!large && split < 8 && tiles * split * 2 <= sms * 2 && g.inner >= 128ull * split) split *= 2;
+  while (!large && split < 8 && tiles * split * 2 <= sms * 4 && g.inner >= 128ull * split) split *= 2;
   const uint32_t inner = (uint32_t)g.inner, each = (uint32_t)(((g.inner + split - 1) / split + 31) / 32 * 32);
-  const float *a = static_cast<const float*>(g.a.p), *b = static_cast<const float*>(g.b.p);
-  const uint64_t ar = g.a_t ? one : g.a.ld, ak = g.a_t ? g.a.ld : one, br = g.b_t ? one : g.b.ld, bk = g.b_t ? g.b.ld : one;
-  const cudaError_t r =
-      large ? launch_kernel(true, gemm_f32_kernel<2, 16>, dim3((unsigned)tiles), 256, 0, st, a, ar, ak, b, br, bk, inner, inner, e)
-            : launch_cluster(gemm_f32_kernel<1, 32>, (unsigned)tiles * split, 256, split, 0, st, a, ar, ak, b, br, bk, inner, each, e);
+  auto operand = [](const Mat& m, bool along, uint64_t rows) {
+    const bool vec = reinterpret_cast<uintptr_t>(m.p) % 16 == 0 && m.ld % 4 == 0;
+    return F32Operand{static_cast<const float*>(m.p), along ? 1 : m.ld, along ? m.ld : 1, (uint32_t)rows, vec ? 1u : 0u};
+  };
+  const F32Operand a = operand(g.a, g.a_t, g.e.rows), b = operand(g.b, g.b_t, g.e.cols);
+  const cudaError_t r = large ? launch_cluster(gemm_f32_kernel<2, 2, 16, 256>, (unsigned)tiles, 256, 1, 0, st, a, b, inner, inner, e)
+                              : launch_cluster(gemm_f32_kernel<2, 1, 32, 128>, (unsigned)tiles * split, 128, split, 0, st, a, b,
+                                               inner, each, e);
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
 
