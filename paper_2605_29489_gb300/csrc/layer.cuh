@@ -74,7 +74,7 @@ struct Elem<__nv_bfloat16> {
   static __device__ __forceinline__ __nv_bfloat16 store(float v) { return __float2bfloat16_rn(v); }
 };
 
-// V consecutive elements as they are stored: 32-bit words of them (8 or 16 bytes, accessed whole), or a single element.
+// V consecutive elements as they are stored: 32-bit words of them (4, 8 or 16 bytes, accessed whole), or a single element.
 // Words, because elements of a struct are moved one by one: a bf16 row's elements then take three or four instructions
 // each to become fp32.
 template <typename T, int V>
@@ -98,8 +98,10 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
     const uint2 u = *reinterpret_cast<const uint2*>(p);
     r.w[0] = u.x;
     r.w[1] = u.y;
+  } else if constexpr (V > 1) {
+    static_assert(V * sizeof(T) == 4, "16, 8 or 4 bytes, or one element");
+    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
   } else {
-    static_assert(V == 1, "16 bytes, 8 bytes or one element");
     r.e = *p;
   }
   return r;
@@ -110,6 +112,8 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) {
     *reinterpret_cast<uint4*>(p) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
   else if constexpr (V * sizeof(T) == 8)
     *reinterpret_cast<uint2*>(p) = make_uint2(v.w[0], v.w[1]);
+  else if constexpr (V > 1)
+    *reinterpret_cast<uint32_t*>(p) = v.w[0];
   else
     *p = v.e;
 }

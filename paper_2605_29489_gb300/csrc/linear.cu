@@ -173,6 +173,33 @@ __device__ __forceinline__ void epi_quad(const Epi<T>& e, uint32_t r, uint32_t c
   store_pack<T, 4>(e.y + r * e.ldy + c, pack<T, 4>(v));
 }
 
+// column c of up to N rows from r on (those below e.rows), the bias already added
+template <typename T, int N>
+__device__ __forceinline__ void epi_column(const Epi<T>& e, uint32_t r, uint32_t c, float* v) {
+  constexpr bool FAST = sizeof(T) == 2;
+  T m[N], s[N];
+  if (e.mul)
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (r + j < e.rows) m[j] = e.mul[(r + (uint64_t)j) * e.ldmul + c];
+  if (e.res)
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (r + j < e.rows) s[j] = e.res[(r + (uint64_t)j) * e.ldres + c];
+  if (e.pre)
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (r + j < e.rows) e.pre[(r + (uint64_t)j) * e.ldpre + c] = Elem<T>::store(v[j]);
+  act_all<FAST, N>(e.act, v);
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (r + j < e.rows) {
+      if (e.mul) v[j] *= Elem<T>::load(m[j]);
+      if (e.res) v[j] += Elem<T>::load(s[j]);
+      e.y[(r + (uint64_t)j) * e.ldy + c] = Elem<T>::store(v[j]);
+    }
+}
+
 // N consecutive columns of a row, from c on (a multiple of N), of which those below e.cols exist
 template <typename T, int N>
 __device__ __forceinline__ void epi_run(const Epi<T>& e, uint32_t r, uint32_t c, float* v) {
@@ -180,13 +207,19 @@ __device__ __forceinline__ void epi_run(const Epi<T>& e, uint32_t r, uint32_t c,
   constexpr bool FAST = sizeof(T) == 2;
   if (r >= e.rows || c >= e.cols) return;
   if (!e.vec || c + N > e.cols) {
+#pragma unroll
     for (int j = 0; j < N; ++j)
       if (c + j < e.cols) {
-        // v[j] without indexing registers by a variable
-        float z = v[0];
+        v[j] += epi_bias(e, c + j);
+        if (e.pre) e.pre[r * e.ldpre + c + j] = Elem<T>::store(v[j]);
+      }
+    act_all<FAST, N>(e.act, v);
 #pragma unroll
-        for (int k = 1; k < N; ++k) z = k == j ? v[k] : z;
-        epi_one(e, r, c + j, z + epi_bias(e, c + j));
+    for (int j = 0; j < N; ++j)
+      if (c + j < e.cols) {
+        if (e.mul) v[j] *= Elem<T>::load(e.mul[r * e.ldmul + c + j]);
+        if (e.res) v[j] += Elem<T>::load(e.res[r * e.ldres + c + j]);
+        e.y[r * e.ldy + c + j] = Elem<T>::store(v[j]);
       }
     return;
   }
@@ -451,7 +484,7 @@ struct Product {
 // tiles of 224 stages on 76 pairs are 3.4 rounds, which took the time of 4), and those of dw fill up what they leave.
 // Bound by the tensor cores: 4096 rows, 4096 -> 14336, 273 us alone (1764 TFLOP/s, cuBLAS 266 in the same call).
 template <bool AT, bool BT, bool TWO>
-__global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constant__ CUtensorMap ma,
+__global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap ma,
                                                             const __grid_constant__ CUtensorMap mb, const Product p1,
                                                             const __grid_constant__ CUtensorMap ma2,
                                                             const __grid_constant__ CUtensorMap mb2, const Product p2,
@@ -592,11 +625,41 @@ __global__ void __launch_bounds__(kGemmThreads) gemm_kernel(const __grid_constan
         return false;
       }
       umma_fence_after();
+      const uint32_t at = tmem + ((quad * 32u) << 16) + half * kTile;
+      if (p.e.vec) {
 #pragma unroll 1
-      for (int j0 = 0; j0 < kTile; j0 += 16) {
-        float v[16];
-        tmem_load16(tmem + ((quad * 32u) << 16) + half * kTile + j0, v);
-        epi_run<bf16, 16>(p.e, (uint32_t)r0 + rank * 128u + row, (uint32_t)(c0 + j0), v);
+        for (int j0 = 0; j0 < kTile; j0 += 16) {
+          float v[16];
+          tmem_load16(at + j0, v);
+          epi_run<bf16, 16>(p.e, (uint32_t)r0 + rank * 128u + row, (uint32_t)(c0 + j0), v);
+        }
+      } else {
+        // rows that are not whole vectors: 32 x 32 sums through shared memory, so that a warp's accesses are along a row
+        // (dw of one row, 2612 x 14201: 500 us element by element down the rows, 309 with one row at a time, 130 with eight)
+        float* turn = reinterpret_cast<float*>(raw + (smem - su32(raw)) + kStages * kStage) + quad * (32 * 33);
+#pragma unroll 1
+        for (int j0 = 0; j0 < kTile; j0 += 32) {
+#pragma unroll
+          for (int h = 0; h < 32; h += 16) {
+            float v[16];
+            tmem_load16(at + j0 + h, v);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) turn[lane * 33 + h + j] = v[j];
+          }
+          __syncwarp();
+          const uint32_t c = (uint32_t)(c0 + j0) + lane, r1 = (uint32_t)r0 + rank * 128u + quad * 32u;
+          if (c < p.e.cols) {
+            const float bias = epi_bias(p.e, c);
+#pragma unroll 1
+            for (uint32_t r = 0; r < 32 && r1 + r < p.e.rows; r += 8) {
+              float v[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = turn[(r + j) * 33 + lane] + bias;
+              epi_column<bf16, 8>(p.e, r1 + r, c, v);
+            }
+          }
+          __syncwarp();
+        }
       }
       umma_fence_before();
       __syncwarp();
@@ -780,17 +843,17 @@ struct CopyArgs {
   uint64_t lds, ldd, rows;
   uint32_t cols;
 };
-// block's share (of `blocks`) of a copy: a warp to a row, four elements of a lane in flight
+// block's share (of `blocks`) of a copy: a warp to a row, 16 elements of a lane in flight
 template <typename T>
 __device__ __forceinline__ void copy_rows(const CopyArgs<T>& m, uint32_t block, uint32_t blocks) {
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   for (uint64_t r = block * 8ull + warp; r < m.rows; r += blocks * 8ull)
-    for (uint32_t c = lane; c < m.cols; c += 128u) {
-      T v[4];
+    for (uint32_t c = lane; c < m.cols; c += 512u) {
+      T v[16];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = m.src && c + 32u * k < m.cols ? m.src[r * m.lds + c + 32u * k] : T(0.0f);
+      for (int k = 0; k < 16; ++k) v[k] = m.src && c + 32u * k < m.cols ? m.src[r * m.lds + c + 32u * k] : T(0.0f);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 16; ++k)
         if (c + 32u * k < m.cols) m.dst[r * m.ldd + c + 32u * k] = v[k];
     }
 }
@@ -816,13 +879,15 @@ struct DzArgs {
 
 // A CTA has 32 V `wide` columns (wide: the warps side by side, 1 to 8) and a run of rows, 8 / wide rows at a time.  Four
 // CTAs to an SM hide what a row waits for better than more rows in flight with fewer: 4096 x 14336, SiLU, three
-// matrices read and one written, 82 us; two rows and three CTAs 94, two and two 114 (a copy of as many bytes takes 76).  The
-// column sums of warps, then of CTAs, are added in order.
+// matrices read and one written, 82 us; two rows and three CTAs 94, two and two 114 (a copy of as many bytes takes 76).  Rows
+// that are no whole vectors go by pairs or single elements, four or eight rows at a time: 5703 x 13418, tanh GELU, 272 us one by
+// one, about 110 by pairs.  The column sums of warps, then of CTAs, are added in order.
 // COPY: some CTAs copy instead.
 template <typename T, int V, int ACT, bool COPY>
 __global__ void __launch_bounds__(256, COPY ? 3 : 4) dz_kernel(const DzArgs<T> p) {
   kernel_begin();
   constexpr bool FAST = sizeof(T) == 2;
+  constexpr int kRows = V * sizeof(T) == 16 ? 1 : V == 1 && sizeof(T) == 2 ? 8 : 4;  // single elements are few bytes: more of them at a time
   __shared__ float sum[8][32 * V + 1], total[8 * 32 * V];
   if (COPY && blockIdx.x >= p.blocks) {
     copy_rows(p.copy[0], blockIdx.x - p.blocks, gridDim.x - p.blocks);
@@ -839,30 +904,42 @@ __global__ void __launch_bounds__(256, COPY ? 3 : 4) dz_kernel(const DzArgs<T> p
   const uint64_t q0 = run * p.rows_each, q1 = q0 + p.rows_each < p.rows ? q0 + p.rows_each : p.rows;
   float s[V] = {};
   if (c < p.cols) {
-    for (uint64_t r = q0 + warp / p.wide; r < q1; r += deep) {
-      const Pack<T, V> dq = load_pack<T, V>(p.dy + r * p.lddy + c);
-      Pack<T, V> zq, mq;
-      if (p.pre) zq = load_pack<T, V>(p.pre + r * p.ldpre + c);
-      if (p.mul) mq = load_pack<T, V>(p.mul + r * p.ldmul + c);
-      float d[V], z[V] = {};
-      unpack(dq, d);
-      if (p.pre) unpack(zq, z);
+    for (uint64_t r0 = q0 + warp / p.wide; r0 < q1; r0 += deep * kRows) {
+      Pack<T, V> dq[kRows], zq[kRows], mq[kRows];
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        float a, g;
-        act_both<ACT, FAST, true>(z[k], a, g);
-        z[k] = d[k] * a;
-        if (ACT != MP_ACT_NONE) d[k] *= g;
-      }
-      if (p.dmul) store_pack<T, V>(p.dmul + r * p.lddmul + c, pack<T, V>(z));
-      if (p.mul) {
-        unpack(mq, z);
-#pragma unroll
-        for (int k = 0; k < V; ++k) d[k] *= z[k];
+      for (int q = 0; q < kRows; ++q) {
+        const uint64_t r = r0 + deep * q;
+        if (r < q1) {
+          dq[q] = load_pack<T, V>(p.dy + r * p.lddy + c);
+          if (p.pre) zq[q] = load_pack<T, V>(p.pre + r * p.ldpre + c);
+          if (p.mul) mq[q] = load_pack<T, V>(p.mul + r * p.ldmul + c);
+        }
       }
 #pragma unroll
-      for (int k = 0; k < V; ++k) s[k] += d[k];
-      if (p.dz) store_pack<T, V>(p.dz + r * p.lddz + c, pack<T, V>(d));
+      for (int q = 0; q < kRows; ++q) {
+        const uint64_t r = r0 + deep * q;
+        if (r < q1) {
+          float d[V], z[V] = {};
+          unpack(dq[q], d);
+          if (p.pre) unpack(zq[q], z);
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            float a, g;
+            act_both<ACT, FAST, true>(z[k], a, g);
+            z[k] = d[k] * a;
+            if (ACT != MP_ACT_NONE) d[k] *= g;
+          }
+          if (p.dmul) store_pack<T, V>(p.dmul + r * p.lddmul + c, pack<T, V>(z));
+          if (p.mul) {
+            unpack(mq[q], z);
+#pragma unroll
+            for (int k = 0; k < V; ++k) d[k] *= z[k];
+          }
+#pragma unroll
+          for (int k = 0; k < V; ++k) s[k] += d[k];
+          if (p.dz) store_pack<T, V>(p.dz + r * p.lddz + c, pack<T, V>(d));
+        }
+      }
     }
   }
   if (!p.db) return;
@@ -1025,7 +1102,7 @@ template <bool AT, bool BT, bool TWO>
 mp_status launch_large(const GemmLaunch& g, const Prepared& a, const Prepared& b, cudaStream_t st) {
   const uint64_t tiles = (uint64_t)a.p.tiles_r * a.p.tiles_c + (TWO ? (uint64_t)b.p.tiles_r * b.p.tiles_c : 0u);
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)device_sms() / 2);
-  const cudaError_t r = launch_cluster(gemm_kernel<AT, BT, TWO>, pairs * 2, kGemmThreads, 2, 6 * 32768 + 1024, st, a.ma, a.mb,
+  const cudaError_t r = launch_cluster(gemm_kernel<AT, BT, TWO>, pairs * 2, kGemmThreads, 2, 6 * 32768 + 4 * 32 * 33 * 4 + 1024, st, a.ma, a.mb,
                                        a.p, b.ma, b.mb, b.p, wait_of(g, std::max(a.p.kb, b.p.kb)));
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
@@ -1175,14 +1252,18 @@ DzPlan dz_plan(const DzLaunch& p, int v) {
   return d;
 }
 
-bool dz_vectors(const DzLaunch& p) {
+// elements to an access: 16 bytes where every row of every matrix allows them, for bf16 else pairs, else one
+int dz_width(const DzLaunch& p) {
   const size_t es = p.dtype == MP_BF16 ? 2 : 4;
-  auto ok = [&](const void* q, uint64_t ld) { return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld * es % 16 == 0); };
-  return p.cols * es % 16 == 0 && ok(p.dy.p, p.dy.ld) && ok(p.pre.p, p.pre.ld) && ok(p.mul.p, p.mul.ld) && ok(p.dz, p.lddz) &&
-         ok(p.dmul, p.lddmul);
+  auto all = [&](size_t unit) {
+    auto ok = [&](const void* q, uint64_t ld) {
+      return !q || (reinterpret_cast<uintptr_t>(q) % unit == 0 && ld * es % unit == 0);
+    };
+    return p.cols * es % unit == 0 && ok(p.dy.p, p.dy.ld) && ok(p.pre.p, p.pre.ld) && ok(p.mul.p, p.mul.ld) && ok(p.dz, p.lddz) &&
+           ok(p.dmul, p.lddmul);
+  };
+  return all(16) ? (int)(16 / es) : es == 2 && all(4) ? 2 : 1;
 }
-
-int dz_width(const DzLaunch& p) { return !dz_vectors(p) ? 1 : p.dtype == MP_BF16 ? 8 : 4; }
 
 // the kernels' arguments of n copies (two at most), and how many CTAs they are for
 template <typename T>
@@ -1281,9 +1362,12 @@ size_t dz_scratch(const DzLaunch& p) {
 }
 
 cudaError_t launch_dz(const DzLaunch& p, const Copy* copies, int n, float* scratch, cudaStream_t st) {
-  const bool vec = dz_vectors(p);
-  if (p.dtype == MP_BF16) return vec ? dz_of<bf16, 8>(p, copies, n, scratch, st) : dz_of<bf16, 1>(p, copies, n, scratch, st);
-  return vec ? dz_of<float, 4>(p, copies, n, scratch, st) : dz_of<float, 1>(p, copies, n, scratch, st);
+  const int v = dz_width(p);
+  if (p.dtype == MP_BF16)
+    return v == 8   ? dz_of<bf16, 8>(p, copies, n, scratch, st)
+           : v == 2 ? dz_of<bf16, 2>(p, copies, n, scratch, st)
+                    : dz_of<bf16, 1>(p, copies, n, scratch, st);
+  return v == 4 ? dz_of<float, 4>(p, copies, n, scratch, st) : dz_of<float, 1>(p, copies, n, scratch, st);
 }
 
 template <typename T>
