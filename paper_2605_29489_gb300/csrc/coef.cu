@@ -5,8 +5,8 @@
 //                       sum_j G[j] * (M_i[j] - M_0[j]),      G = dL / dM_A.
 //
 // Bound by memory: G and the base are read once for all experts of a block, an expert's block only where
-// the mask has it, and blocks that no expert is read from not at all.  An item is kItemVecs 16-byte vectors
-// of one block; a thread keeps its vectors of G and of the base while the experts of the mask stream
+// the mask has it, and blocks that no expert is read from not at all.  An item is one or four rounds of a
+// CTA's 16-byte vectors of one block; a thread keeps its vectors of G and of the base while the experts of the mask stream
 // past, the next expert's loads in flight.  Differences and products are fp32 sums of 64 elements
 // per thread, then trees over lanes and warps; the items' sums are added in fp64 in a fixed order.
 #include <algorithm>
@@ -19,12 +19,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVecs = 2;                              // vectors a thread keeps at a time
-constexpr uint32_t kItemVecs = kThreads * kVecs * 4;  // an item: four rounds of those
-
-template <typename T>
-constexpr uint32_t item_elems() {
-  return kItemVecs * Elem<T>::kVec;
-}
+constexpr uint32_t kRounds = 4;                       // rounds of those in an item, where items are plenty
 
 // element e of a 16-byte vector as fp32
 template <typename T>
@@ -58,18 +53,17 @@ __device__ __forceinline__ uint4 load_vec(const T* p, uint32_t v, uint32_t n) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 4) coef_kernel(const CoefLaunch p, float* part, uint32_t per_block) {
+__global__ void __launch_bounds__(kThreads, 4) coef_kernel(const CoefLaunch p, float* part, uint32_t per_block, uint32_t item) {
   kernel_begin();
   constexpr int V = Elem<T>::kVec;
   __shared__ float sum[kThreads / 32][kMaxK];
-  const uint64_t item = blockIdx.x, n_items = gridDim.x;
-  const uint64_t b = item / per_block;
-  const uint32_t at = (uint32_t)(item % per_block) * item_elems<T>();
+  const uint64_t n_items = gridDim.x, b = blockIdx.x / per_block;
+  const uint32_t at = blockIdx.x % per_block * item;  // item: elements of one
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   const uint32_t len = p.blk_len[b];
   uint32_t mask = at < len ? p.mask[b] : 0u;
   const uint64_t off = p.blk_off[b] + at;
-  const uint32_t n = at < len ? (len - at < item_elems<T>() ? len - at : item_elems<T>()) : 0u;
+  const uint32_t n = at < len ? min(len - at, item) : 0u;
   if (kChecked && !chunk_in_bounds(b, 0, p.n_blocks, p.blk_off[b], len, off, n, mask, p.K, sizeof(T), 0, p.ext)) {
     if (threadIdx.x == 0) atomicOr_system(p.err, kErrBounds);
     mask = 0u;
@@ -125,7 +119,7 @@ __global__ void __launch_bounds__(kThreads, 4) coef_kernel(const CoefLaunch p, f
     float s = 0.0f;
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) s += sum[w][threadIdx.x];
-    part[threadIdx.x * n_items + item] = s;
+    part[threadIdx.x * n_items + blockIdx.x] = s;
   }
 }
 
@@ -152,10 +146,14 @@ __global__ void __launch_bounds__(kThreads) coef_sum_kernel(const float* part, u
   }
 }
 
-uint32_t items_per_block(const CoefLaunch& p) {
-  const uint32_t e = p.dtype == MP_BF16 ? item_elems<__nv_bfloat16>() : item_elems<float>();
-  return (p.block_elems + e - 1) / e;
+// Elements of an item: four rounds of a CTA; one where four-round items would not give each of 1,024 CTAs (four to an SM and
+// a second lot) one of its own: a CTA's experts stream past one after the other, so that 16 of them over 1.8M elements in
+// blocks of 65,536 took 51 us with four rounds, 26 with one.
+uint32_t item_elems(const CoefLaunch& p) {
+  const uint32_t round = kThreads * kVecs * (p.dtype == MP_BF16 ? 8u : 4u), item = round * kRounds;
+  return p.n_blocks * ((p.block_elems + item - 1) / item) < 1024 ? round : item;
 }
+uint32_t items_per_block(const CoefLaunch& p) { return (p.block_elems + item_elems(p) - 1) / item_elems(p); }
 
 }  // namespace
 
@@ -167,8 +165,8 @@ cudaError_t launch_coef(const CoefLaunch& p, float* part, cudaStream_t st) {
   if (items > 0x7FFFFFFFull) return cudaErrorInvalidValue;
   const dim3 grid((unsigned)items);
   cudaError_t e = p.dtype == MP_BF16
-                      ? launch_kernel(true, coef_kernel<__nv_bfloat16>, grid, kThreads, 0, st, p, part, per_block)
-                      : launch_kernel(true, coef_kernel<float>, grid, kThreads, 0, st, p, part, per_block);
+                      ? launch_kernel(true, coef_kernel<__nv_bfloat16>, grid, kThreads, 0, st, p, part, per_block, item_elems(p))
+                      : launch_kernel(true, coef_kernel<float>, grid, kThreads, 0, st, p, part, per_block, item_elems(p));
   if (e != cudaSuccess) return e;
   return launch_kernel(true, coef_sum_kernel, dim3(p.n_tensors, p.K), kThreads, 0, st, (const float*)part, items,
                        per_block, p.t_blk0, p.n_tensors, p.out);

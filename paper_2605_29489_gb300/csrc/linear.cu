@@ -173,7 +173,7 @@ __device__ __forceinline__ void epi_quad(const Epi<T>& e, uint32_t r, uint32_t c
   store_pack<T, 4>(e.y + r * e.ldy + c, pack<T, 4>(v));
 }
 
-// column c of up to N rows from r on (those below e.rows), the bias already added
+// column c of N rows, r and every second after it (those below e.rows), the bias already added
 template <typename T, int N>
 __device__ __forceinline__ void epi_column(const Epi<T>& e, uint32_t r, uint32_t c, float* v) {
   constexpr bool FAST = sizeof(T) == 2;
@@ -181,22 +181,22 @@ __device__ __forceinline__ void epi_column(const Epi<T>& e, uint32_t r, uint32_t
   if (e.mul)
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (r + j < e.rows) m[j] = e.mul[(r + (uint64_t)j) * e.ldmul + c];
+      if (r + 2 * j < e.rows) m[j] = e.mul[(r + 2ull * j) * e.ldmul + c];
   if (e.res)
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (r + j < e.rows) s[j] = e.res[(r + (uint64_t)j) * e.ldres + c];
+      if (r + 2 * j < e.rows) s[j] = e.res[(r + 2ull * j) * e.ldres + c];
   if (e.pre)
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (r + j < e.rows) e.pre[(r + (uint64_t)j) * e.ldpre + c] = Elem<T>::store(v[j]);
+      if (r + 2 * j < e.rows) e.pre[(r + 2ull * j) * e.ldpre + c] = Elem<T>::store(v[j]);
   act_all<FAST, N>(e.act, v);
 #pragma unroll
   for (int j = 0; j < N; ++j)
-    if (r + j < e.rows) {
+    if (r + 2 * j < e.rows) {
       if (e.mul) v[j] *= Elem<T>::load(m[j]);
       if (e.res) v[j] += Elem<T>::load(s[j]);
-      e.y[(r + (uint64_t)j) * e.ldy + c] = Elem<T>::store(v[j]);
+      e.y[(r + 2ull * j) * e.ldy + c] = Elem<T>::store(v[j]);
     }
 }
 
@@ -261,8 +261,10 @@ __device__ __forceinline__ void epi_run(const Epi<T>& e, uint32_t r, uint32_t c,
 
 constexpr int kBK = 64;                 // inner elements of a stage: one 128-byte swizzle span of bf16
 constexpr uint32_t kBoxT = 8192;        // bytes of an mn-major box: 64 k x 64 mn
-constexpr uint32_t kWarps = 6;
+constexpr uint32_t kWarps = 6;          // of split_kernel
 constexpr int kGemmThreads = 32 * kWarps;       // a TMA warp, a warp that issues products, four epilogue warps
+constexpr uint32_t kEpiWarps = 8;       // epilogue warps of gemm_kernel: two to each quarter of the tensor memory's lanes
+constexpr int kLargeThreads = 32 * (2 + kEpiWarps);
 
 using bf16 = __nv_bfloat16;
 
@@ -484,7 +486,7 @@ struct Product {
 // tiles of 224 stages on 76 pairs are 3.4 rounds, which took the time of 4), and those of dw fill up what they leave.
 // Bound by the tensor cores: 4096 rows, 4096 -> 14336, 273 us alone (1764 TFLOP/s, cuBLAS 266 in the same call).
 template <bool AT, bool BT, bool TWO>
-__global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap ma,
+__global__ void __launch_bounds__(kLargeThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap ma,
                                                             const __grid_constant__ CUtensorMap mb, const Product p1,
                                                             const __grid_constant__ CUtensorMap ma2,
                                                             const __grid_constant__ CUtensorMap mb2, const Product p2,
@@ -507,7 +509,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&acc_full[s], 1);
-      mbar_init(&acc_empty[s], 2 * 4);
+      mbar_init(&acc_empty[s], 2 * kEpiWarps);
     }
     mbar_fence_init();
     abort = 0;
@@ -614,7 +616,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       mbar_wait_drain(&acc_full[n & 1u], (n >> 1) & 1u);
     }
   } else if (warp >= 2) {
-    const uint32_t quad = warp & 3u, row = quad * 32u + lane;
+    // this warp's lanes of tensor memory, and its half of the columns
+    const uint32_t quad = warp & 3u, row = quad * 32u + lane, first = (warp - 2) / 4 * (kTile / 2);
     uint32_t n = 0;
     for_tiles([&](auto, const Product& p, uint32_t t) {
       const uint32_t half = n & 1u;
@@ -628,34 +631,32 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       const uint32_t at = tmem + ((quad * 32u) << 16) + half * kTile;
       if (p.e.vec) {
 #pragma unroll 1
-        for (int j0 = 0; j0 < kTile; j0 += 16) {
-          float v[16];
-          tmem_load16(at + j0, v);
-          epi_run<bf16, 16>(p.e, (uint32_t)r0 + rank * 128u + row, (uint32_t)(c0 + j0), v);
+        for (uint32_t j0 = first; j0 < first + kTile / 2; j0 += 32) {
+          float v[32];
+          tmem_load32(at + j0, v);
+          epi_run<bf16, 16>(p.e, (uint32_t)r0 + rank * 128u + row, (uint32_t)c0 + j0, v);
+          epi_run<bf16, 16>(p.e, (uint32_t)r0 + rank * 128u + row, (uint32_t)c0 + j0 + 16, v + 16);
         }
       } else {
-        // rows that are not whole vectors: 32 x 32 sums through shared memory, so that a warp's accesses are along a row
+        // rows that are not whole vectors: 32 x 16 sums through shared memory, so that a warp's accesses are along two rows
         // (dw of one row, 2612 x 14201: 500 us element by element down the rows, 309 with one row at a time, 130 with eight)
-        float* turn = reinterpret_cast<float*>(raw + (smem - su32(raw)) + kStages * kStage) + quad * (32 * 33);
+        float* turn = reinterpret_cast<float*>(raw + (smem - su32(raw)) + kStages * kStage) + (warp - 2) * (32 * 17);
 #pragma unroll 1
-        for (int j0 = 0; j0 < kTile; j0 += 32) {
+        for (uint32_t j0 = first; j0 < first + kTile / 2; j0 += 16) {
+          float v[16];
+          tmem_load16(at + j0, v);
 #pragma unroll
-          for (int h = 0; h < 32; h += 16) {
-            float v[16];
-            tmem_load16(at + j0 + h, v);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) turn[lane * 33 + h + j] = v[j];
-          }
+          for (int j = 0; j < 16; ++j) turn[lane * 17 + j] = v[j];
           __syncwarp();
-          const uint32_t c = (uint32_t)(c0 + j0) + lane, r1 = (uint32_t)r0 + rank * 128u + quad * 32u;
+          const uint32_t c = (uint32_t)c0 + j0 + (lane & 15u), up = lane >> 4, r1 = (uint32_t)r0 + rank * 128u + quad * 32u;
           if (c < p.e.cols) {
             const float bias = epi_bias(p.e, c);
 #pragma unroll 1
-            for (uint32_t r = 0; r < 32 && r1 + r < p.e.rows; r += 8) {
-              float v[8];
+            for (uint32_t r = up; r < 32 && r1 + r < p.e.rows; r += 16) {
+              float z[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = turn[(r + j) * 33 + lane] + bias;
-              epi_column<bf16, 8>(p.e, r1 + r, c, v);
+              for (int j = 0; j < 8; ++j) z[j] = turn[(r + 2 * j) * 17 + (lane & 15u)] + bias;
+              epi_column<bf16, 8>(p.e, r1 + r, c, z);
             }
           }
           __syncwarp();
@@ -1102,7 +1103,7 @@ template <bool AT, bool BT, bool TWO>
 mp_status launch_large(const GemmLaunch& g, const Prepared& a, const Prepared& b, cudaStream_t st) {
   const uint64_t tiles = (uint64_t)a.p.tiles_r * a.p.tiles_c + (TWO ? (uint64_t)b.p.tiles_r * b.p.tiles_c : 0u);
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)device_sms() / 2);
-  const cudaError_t r = launch_cluster(gemm_kernel<AT, BT, TWO>, pairs * 2, kGemmThreads, 2, 6 * 32768 + 4 * 32 * 33 * 4 + 1024, st, a.ma, a.mb,
+  const cudaError_t r = launch_cluster(gemm_kernel<AT, BT, TWO>, pairs * 2, kLargeThreads, 2, 6 * 32768 + kEpiWarps * 32 * 17 * 4 + 1024, st, a.ma, a.mb,
                                        a.p, b.ma, b.mb, b.p, wait_of(g, std::max(a.p.kb, b.p.kb)));
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
