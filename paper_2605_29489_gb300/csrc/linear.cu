@@ -200,6 +200,98 @@ __device__ __forceinline__ void epi_column(const Epi<T>& e, uint32_t r, uint32_t
     }
 }
 
+// The epilogue of 32 rows (r0 + lane) x 32 columns (from c on, a multiple of 32) by a warp, from columns tmem of its tensor memory.  Memory is
+// accessed along the rows, eight rows of 64 bytes at a time, and turns in buf (32 rows of kTurn bytes): a lane's own row
+// would be 32 lines and half sectors to an access (dw of 240 rows, 12088 x 3992, 64 us instead of PLACEHOLDER).
+constexpr uint32_t kTurn = 80;
+__device__ __forceinline__ void epi_block(const Epi<__nv_bfloat16>& e, uint32_t r0, uint32_t c, uint32_t lane,
+                                          uint32_t tmem, uint8_t* buf) {
+  using T = __nv_bfloat16;
+  const uint32_t up = lane / 4, ch = lane % 4 * 8;  // of the accesses along the rows: row up + 8 i, columns c + ch ...
+  const uint32_t n = c + ch < e.cols ? min(8u, e.cols - c - ch) : 0u;
+  if (c >= e.cols) return;
+  // the factor and the residual are on their way before anything else
+  Pack<T, 8> m[4], s[4];
+  auto fetch = [&](const T* p, uint64_t ld, Pack<T, 8>* to) {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      const uint32_t r = r0 + up + 8 * i;
+      const T* src = p + r * ld + c + ch;
+      if (r < e.rows) {
+        if (n == 8) {
+          to[i] = load_pack<T, 8>(src);
+        } else {
+          float f[8] = {};
+#pragma unroll
+          for (uint32_t k = 0; k < 8; ++k)
+            if (k < n) f[k] = Elem<T>::load(src[k]);
+          to[i] = pack<T, 8>(f);
+        }
+      }
+    }
+  };
+  auto turn = [&](const Pack<T, 8>* from, float* to) {
+    __syncwarp();
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) store_pack<T, 8>(reinterpret_cast<T*>(buf + (up + 8 * i) * kTurn) + ch, from[i]);
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) unpack(load_pack<T, 8>(reinterpret_cast<const T*>(buf + lane * kTurn) + 8 * q), to + 8 * q);
+  };
+  if (e.mul) fetch(e.mul, e.ldmul, m);
+  if (e.res) fetch(e.res, e.ldres, s);
+  float v[32];
+  tmem_load32(tmem, v);
+  auto write = [&](T* m, uint64_t ld, const float* from) {
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) store_pack<T, 8>(reinterpret_cast<T*>(buf + lane * kTurn) + 8 * q, pack<T, 8>(from + 8 * q));
+    __syncwarp();
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      const uint32_t r = r0 + up + 8 * i;
+      T* dst = m + r * ld + c + ch;
+      const T* src = reinterpret_cast<const T*>(buf + (up + 8 * i) * kTurn) + ch;
+      if (r < e.rows) {
+        if (n == 8)
+          store_pack<T, 8>(dst, load_pack<T, 8>(src));
+        else
+          for (uint32_t k = 0; k < n; ++k) dst[k] = src[k];
+      }
+    }
+  };
+  if (e.bias) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float u[8];
+      if (c + 8 * q + 8 <= e.cols) {
+        unpack(load_pack<T, 8>(e.bias + c + 8 * q), u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[8 * q + k] += u[k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (c + 8 * q + k < e.cols) v[8 * q + k] += Elem<T>::load(e.bias[c + 8 * q + k]);
+      }
+    }
+  }
+  if (e.pre) write(e.pre, e.ldpre, v);
+  act_all<true, 32>(e.act, v);
+  if (e.mul) {
+    float u[32];
+    turn(m, u);
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] *= u[k];
+  }
+  if (e.res) {
+    float u[32];
+    turn(s, u);
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] += u[k];
+  }
+  write(e.y, e.ldy, v);
+}
+
 // N consecutive columns of a row, from c on (a multiple of N), of which those below e.cols exist
 template <typename T, int N>
 __device__ __forceinline__ void epi_run(const Epi<T>& e, uint32_t r, uint32_t c, float* v) {
@@ -617,7 +709,9 @@ __global__ void __launch_bounds__(kLargeThreads, 1) gemm_kernel(const __grid_con
     }
   } else if (warp >= 2) {
     // this warp's lanes of tensor memory, and its half of the columns
-    const uint32_t quad = warp & 3u, row = quad * 32u + lane, first = (warp - 2) / 4 * (kTile / 2);
+    const uint32_t quad = warp & 3u, first = (warp - 2) / 4 * (kTile / 2);
+    uint8_t* own = raw + (smem - su32(raw)) + kStages * kStage + (warp - 2) * (32 * kTurn);
+    static_assert(kTurn >= 17 * 4, "either way to turn sums fits");
     uint32_t n = 0;
     for_tiles([&](auto, const Product& p, uint32_t t) {
       const uint32_t half = n & 1u;
@@ -632,15 +726,12 @@ __global__ void __launch_bounds__(kLargeThreads, 1) gemm_kernel(const __grid_con
       if (p.e.vec) {
 #pragma unroll 1
         for (uint32_t j0 = first; j0 < first + kTile / 2; j0 += 32) {
-          float v[32];
-          tmem_load32(at + j0, v);
-          epi_run<bf16, 16>(p.e, (uint32_t)r0 + rank * 128u + row, (uint32_t)c0 + j0, v);
-          epi_run<bf16, 16>(p.e, (uint32_t)r0 + rank * 128u + row, (uint32_t)c0 + j0 + 16, v + 16);
+          epi_block(p.e, (uint32_t)r0 + rank * 128u + quad * 32u, (uint32_t)c0 + j0, lane, at + j0, own);
         }
       } else {
         // rows that are not whole vectors: 32 x 16 sums through shared memory, so that a warp's accesses are along two rows
         // (dw of one row, 2612 x 14201: 500 us element by element down the rows, 309 with one row at a time, 130 with eight)
-        float* turn = reinterpret_cast<float*>(raw + (smem - su32(raw)) + kStages * kStage) + (warp - 2) * (32 * 17);
+        float* turn = reinterpret_cast<float*>(own);
 #pragma unroll 1
         for (uint32_t j0 = first; j0 < first + kTile / 2; j0 += 16) {
           float v[16];
@@ -1103,7 +1194,7 @@ template <bool AT, bool BT, bool TWO>
 mp_status launch_large(const GemmLaunch& g, const Prepared& a, const Prepared& b, cudaStream_t st) {
   const uint64_t tiles = (uint64_t)a.p.tiles_r * a.p.tiles_c + (TWO ? (uint64_t)b.p.tiles_r * b.p.tiles_c : 0u);
   const unsigned pairs = (unsigned)std::min<uint64_t>(tiles, (uint64_t)device_sms() / 2);
-  const cudaError_t r = launch_cluster(gemm_kernel<AT, BT, TWO>, pairs * 2, kLargeThreads, 2, 6 * 32768 + kEpiWarps * 32 * 17 * 4 + 1024, st, a.ma, a.mb,
+  const cudaError_t r = launch_cluster(gemm_kernel<AT, BT, TWO>, pairs * 2, kLargeThreads, 2, 6 * 32768 + kEpiWarps * 32 * kTurn + 1024, st, a.ma, a.mb,
                                        a.p, b.ma, b.mb, b.p, wait_of(g, std::max(a.p.kb, b.p.kb)));
   return r == cudaSuccess ? MP_OK : cuda_fail(r, "linear kernel");
 }
