@@ -70,8 +70,9 @@ struct Args {
       if (x.rows > 1 && x.rows - 1 > (1ull << 56) / es / x.ld) return refuse(std::string(x.name) + " is too large");
       if (x.ld > (1ull << 38) / es) return refuse(std::string(x.name) + ": its row stride is too large");
       if (reinterpret_cast<uintptr_t>(x.p) % es != 0) return refuse(std::string(x.name) + " is not aligned to its elements");
-      if (!device_pointer(x.p)) return refuse(std::string(x.name) + " must be device memory");
     }
+    for (int k = 0; k < n; ++k)
+      if (!device_pointer(a[k].p)) return refuse(std::string(a[k].name) + " must be device memory");
     for (int k = 0; k < n; ++k) {
       if (!a[k].out) continue;
       for (int q = 0; q < n; ++q) {

@@ -6,11 +6,13 @@
 //
 // bf16 operands go to the tensor cores (tcgen05), accumulated in fp32 in tensor memory: TMA brings the
 // tiles, whichever way the operand is stored (the three products need x and w both along and across
-// their rows), one thread issues the products, four warps take the sums through the epilogue.
+// their rows), one warp issues the products, four or eight take the sums through the epilogue.
 // What lies past an edge is read as zeros and not written.  Two kernels:
 //
 //   gemm_kernel   tiles of 256 x 256 by pairs of CTAs, persistent: while the epilogue of one tile runs, the
-//                 products of the next fill the other half of tensor memory.  Bound by the tensor cores.
+//                 products of the next fill the other half of tensor memory.  Bound by the tensor cores.  Taken from 129
+//                 rows and half as many tiles as SM pairs on: 2048 x 2048 x 1024 rows, 32 tiles, 14.2 us split and 15.5 by
+//                 large tiles, 4096 x 4096 x 777 rows, 64 tiles, 31.5 and 24.9.
 //   split_kernel  tiles of 128 features x up to 128 rows, the inner dimension split over the CTAs of a
 //                 cluster, whose sums are added over distributed shared memory in the order of the CTAs (no
 //                 scratch, no atomics, one launch).  For few rows, where the weights' bytes are the work
@@ -36,7 +38,8 @@ namespace {
 // normal distribution function; its tanh form: p = (1 + tanh(u)) / 2 = sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3),
 // which keeps its relative accuracy where 1 + tanh cancels.  FAST: bf16 results, where the fast exponential's 2 ulp
 // do not show, nor the 1.5e-7 by which Abramowitz and Stegun's 7.1.26 is off erf; its exponential is the one that
-// the derivative needs.  (4096 x 14336, the backward pass's elementwise part: GELU 130 us with erff, tanh 119 with tanhf, SiLU 82.)
+// the derivative needs.  (4096 x 14336, the backward pass's elementwise part: GELU 130 us with erff and 94 so, its tanh
+// form 119 with tanhf and 94, SiLU 80.)
 template <bool FAST>
 __device__ __forceinline__ float exp_of(float z) {
   return FAST ? __expf(z) : expf(z);
@@ -202,7 +205,7 @@ __device__ __forceinline__ void epi_column(const Epi<T>& e, uint32_t r, uint32_t
 
 // The epilogue of 32 rows (r0 + lane) x 32 columns (from c on, a multiple of 32) by a warp, from columns tmem of its tensor memory.  Memory is
 // accessed along the rows, eight rows of 64 bytes at a time, and turns in buf (32 rows of kTurn bytes): a lane's own row
-// would be 32 lines and half sectors to an access (dw of 240 rows, 12088 x 3992, 64 us instead of PLACEHOLDER).
+// would be 32 lines and half sectors to an access (gradients of 186 rows, 7296 -> 13672, 197 us instead of 177).
 constexpr uint32_t kTurn = 80;
 __device__ __forceinline__ void epi_block(const Epi<__nv_bfloat16>& e, uint32_t r0, uint32_t c, uint32_t lane,
                                           uint32_t tmem, uint8_t* buf) {
