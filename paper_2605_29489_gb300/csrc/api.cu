@@ -353,11 +353,10 @@ void scratch_free(void* p, cudaStream_t st) {
 bool device_pointer(const void* p) { return is_device_ptr(p); }
 
 uint32_t* layer_error_word() {
-  static uint32_t* const word = [] {
-    uint32_t* w = static_cast<uint32_t*>(pin_get(256));
-    if (w) *w = 0;
-    return w;
-  }();
+  static std::mutex mu;
+  static uint32_t* word = nullptr;
+  std::lock_guard<std::mutex> lk(mu);
+  if (!word && (word = static_cast<uint32_t*>(pin_get(256)))) *word = 0;
   return word;
 }
 
@@ -1554,12 +1553,13 @@ mp_status coef_grad(const mp_family* family, const mp_index* index, const mp_pla
   if (!now_captured && (e = done.make()) != cudaSuccess) return cuda_fail(e, "event");
   Scratch s;
   if ((e = s.get(coef_scratch(p), cs)) != cudaSuccess) return cuda_fail(e, "scratch");
-  if ((e = launch_coef(p, static_cast<float*>(s.p), cs)) != cudaSuccess) return cuda_fail(e, "coefficient kernels");
-  if (now_captured) return MP_OK;
-  if ((e = cudaEventRecord(done.get(), cs)) != cudaSuccess) return cuda_fail(e, "event record");
-  index->users.add(done);
-  plan->users.add(done);
-  return MP_OK;
+  const cudaError_t launched = launch_coef(p, static_cast<float*>(s.p), cs);
+  if (!now_captured) {  // whatever was enqueued reads the handles until then
+    if ((e = cudaEventRecord(done.get(), cs)) != cudaSuccess) return cuda_fail(e, "event record");
+    index->users.add(done);
+    plan->users.add(done);
+  }
+  return launched == cudaSuccess ? MP_OK : cuda_fail(launched, "coefficient kernels");
 }
 
 mp_status layer_status(mp_stream stream) {

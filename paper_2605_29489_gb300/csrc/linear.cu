@@ -1064,7 +1064,7 @@ using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, 
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// the driver's encoder, found in the driver's library at the first use (the library itself links no driver)
+// the encoder of tensor maps, from libcuda at its first use (the library itself does not link libcuda)
 EncodeTiled encode_tiled() {
   static const EncodeTiled f = [] {
     void* so = dlopen("libcuda.so.1", RTLD_NOW);
@@ -1077,7 +1077,7 @@ EncodeTiled encode_tiled() {
 mp_status make_map(CUtensorMap* map, const Mat& m, bool t, uint64_t n, uint64_t inner, uint32_t box) {
   const EncodeTiled f = encode_tiled();
   if (!f) {
-    set_static_error("the driver's tensor-map encoder is not available");
+    set_static_error("the CUDA driver's tensor-map encoder is not available");
     return MP_ERR_CUDA;
   }
   const cuuint64_t dims[2] = {t ? n : inner, t ? inner : n};
@@ -1087,7 +1087,7 @@ mp_status make_map(CUtensorMap* map, const Mat& m, bool t, uint64_t n, uint64_t 
                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
-    set_static_error("the driver refused a matrix (cuTensorMapEncodeTiled)");
+    set_static_error("cuTensorMapEncodeTiled refused a matrix");
     return MP_ERR_CUDA;
   }
   return MP_OK;

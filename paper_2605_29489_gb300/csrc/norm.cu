@@ -24,9 +24,11 @@ namespace {
 constexpr uint32_t kWideCols = 8192;    // the widest row of the backward pass with sums in registers
 constexpr uint32_t kNormCols = 16384;   // the widest row of the forward pass in registers
 
+// the sum over N lanes next to each other (a power of two)
+template <int N = 32>
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  for (int o = N / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   return v;
 }
 
@@ -35,8 +37,9 @@ __device__ __forceinline__ float warp_sum(float v) {
 // through the same tree in each warp.
 template <int ROWT, bool TWO, int WARPS>
 __device__ __forceinline__ float2 row_sum(float a, float b, float2 (*red)[WARPS], uint32_t& turn) {
-  a = warp_sum(a);
-  if (TWO) b = warp_sum(b);
+  constexpr int kLanes = ROWT < 32 ? ROWT : 32;
+  a = warp_sum<kLanes>(a);
+  if (TWO) b = warp_sum<kLanes>(b);
   if constexpr (ROWT > 32) {
     constexpr int W = ROWT / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = (threadIdx.x / ROWT) * W;
@@ -224,7 +227,7 @@ constexpr int backward_vecs() {
 // dx of the rows of a CTA and its sums for dw (part [2 * cta]) and db (part [2 * cta + 1]).  The next row's loads are on
 // their way while this one's sums are taken.
 template <typename T, int V, int ROWT, bool LAYER>
-__global__ void __launch_bounds__(cta_of<ROWT>(), (ROWT == 32 ? 3 : 4) * backward_threads<T, V>() / 4 / cta_of<ROWT>())
+__global__ void __launch_bounds__(cta_of<ROWT>(), (ROWT <= 32 ? 3 : 4) * backward_threads<T, V>() / 4 / cta_of<ROWT>())
     norm_backward_kernel(const NormLaunch p, float* part) {
   kernel_begin();
   constexpr int NV = backward_vecs<T, V>(), kRows = cta_of<ROWT>() / ROWT;
@@ -338,12 +341,13 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), (ROWT == 32 ? 3 : 4) * backwar
   }
 }
 
-// The same for many rows of whole 16-byte vectors: bulk copies bring them, ring slots of an x, a dy and an add row each, so that an
-// SM has about 200 KB on their way at any time, whatever its threads wait for: RMS norm 4096 x 4096 with add, 41 us with
-// the next row in registers (48 KB an SM), 28 with the ring
-// (4.8 TB/s).  A producer warp fills the slots in the order of the rows;
-// groups of ROWT threads, 16 columns each, take the rows in turn.  The groups' sums are added up in shared memory:
-// one part per CTA.
+// The same for many long rows of whole 16-byte vectors: bulk copies bring them, ring slots of an x, a dy and an add row each, so
+// that an SM has up to 200 KB on their way, whatever its threads wait for.  A producer warp fills the slots in the order of the
+// rows; groups of ROWT threads, 16 columns each, take the rows in turn.  The groups' sums are added up in shared memory: one
+// part per CTA.  A row costs about 0.45 us of an SM besides its bytes, so that rows have to be long, and layer norms, whose two
+// sums per column leave the other kernel few registers, gain most (both sides in us, bf16 unless stated, 67 MB each of x and dy):
+// rows of 4 KB RMS 47 without and 60 with the ring, layer 71 and 65, fp32 layer with add 97 and 62; rows of 8 KB RMS with add 55 and
+// 53, layer 73 and 58, fp32 RMS with add 57 and 51.
 constexpr int kRingThreads = 512 + 32, kRingSlots = 16;
 template <typename T, int ROWT, bool LAYER>
 __global__ void __launch_bounds__(kRingThreads, 1) norm_backward_ring_kernel(const NormLaunch p, float* part, uint32_t slots,
@@ -633,20 +637,23 @@ int sm_count() {
   return n;
 }
 
-// threads per row: the vectors of a row over NV per thread
+// threads per row: the vectors of a row over NV per thread; eight for the rows of attention heads, four to a warp
 template <int V, int NV>
 int threads_for(uint32_t cols) {
   const uint32_t need = (cols + V * NV - 1) / (V * NV);
-  return need <= 32 ? 32 : need <= 128 ? 128 : need <= 256 ? 256 : need <= 512 ? 512 : 1024;
+  return need <= 8 ? 8 : need <= 32 ? 32 : need <= 128 ? 128 : need <= 256 ? 256 : need <= 512 ? 512 : 1024;
 }
+
+uint64_t rows_to_cta(int t) { return t < 128 ? 128u / (uint32_t)t : 1u; }
 
 template <typename T, int V, int NV, bool LAYER>
 cudaError_t norm_forward(const NormLaunch& p, cudaStream_t st) {
   const int t = threads_for<V, NV>(p.cols);
-  const uint64_t ctas = t == 32 ? (p.rows + 3) / 4 : p.rows;
+  const uint64_t ctas = (p.rows + rows_to_cta(t) - 1) / rows_to_cta(t);
   const uint64_t most = (uint64_t)sm_count() * (kForward / std::max(t, 128));
   const dim3 grid((unsigned)std::min(ctas, most));
   switch (t) {
+    case 8: return launch_kernel(true, norm_kernel<T, V, NV, 8, LAYER>, grid, 128, 0, st, p);
     case 32: return launch_kernel(true, norm_kernel<T, V, NV, 32, LAYER>, grid, 128, 0, st, p);
     case 128: return launch_kernel(true, norm_kernel<T, V, NV, 128, LAYER>, grid, 128, 0, st, p);
     case 256: return launch_kernel(true, norm_kernel<T, V, NV, 256, LAYER>, grid, 256, 0, st, p);
@@ -671,11 +678,12 @@ cudaError_t norm_forward_of(const NormLaunch& p, cudaStream_t st) {
 template <typename T, int V>
 uint32_t backward_ctas(const NormLaunch& p) {
   const int t = threads_for<V, backward_vecs<T, V>()>(p.cols);
-  const uint64_t ctas = t == 32 ? (p.rows + 3) / 4 : p.rows;
-  return (uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * ((t == 32 ? 3 : 4) * backward_threads<T, V>() / 4 / std::max(t, 128)));
+  const uint64_t ctas = (p.rows + rows_to_cta(t) - 1) / rows_to_cta(t);
+  return (uint32_t)std::min<uint64_t>(ctas, (uint64_t)sm_count() * ((t <= 32 ? 3 : 4) * backward_threads<T, V>() / 4 / std::max(t, 128)));
 }
 
-// The ring: rows of 2 KB or more of whole vectors, four or more to an SM (fewer do not fill the ring twice); 0 slots: not.
+// The ring: rows of whole vectors, of 8 KB or more, or 4 KB for layer norms; four or more to an SM (fewer do not fill the ring twice);
+// 0 slots: not.
 struct RingPlan {
   uint32_t slots, slot_bytes, ctas;
 };
@@ -683,7 +691,7 @@ RingPlan ring_plan(const NormLaunch& p) {
   const uint32_t es = p.dtype == MP_BF16 ? 2 : 4, row = p.cols * es, slot = (p.add ? 3u : 2u) * row;
   const int sms = sm_count();
   RingPlan r{0, slot, (uint32_t)sms};
-  if (p.cols > kWideCols || row < 2048 || row % 16 != 0 || p.rows < 4ull * sms) return r;
+  if (p.cols > kWideCols || row < (p.layer ? 4096u : 8192u) || row % 16 != 0 || p.rows < 4ull * sms) return r;
   if (!row16(p.x, p.ldx, es) || !row16(p.dy, p.lddy, es) || !row16(p.add, p.ldadd, es) || !row16(p.dx, p.lddx, es) ||
       !row16(p.weight, 0, es))
     return r;
@@ -721,6 +729,7 @@ template <typename T, int V, bool LAYER>
 cudaError_t norm_backward_rows(const NormLaunch& p, float* part, cudaStream_t st) {
   const dim3 grid(backward_ctas<T, V>(p));
   switch (threads_for<V, backward_vecs<T, V>()>(p.cols)) {
+    case 8: return launch_kernel(true, norm_backward_kernel<T, V, 8, LAYER>, grid, 128, 0, st, p, part);
     case 32: return launch_kernel(true, norm_backward_kernel<T, V, 32, LAYER>, grid, 128, 0, st, p, part);
     case 128: return launch_kernel(true, norm_backward_kernel<T, V, 128, LAYER>, grid, 128, 0, st, p, part);
     case 256: return launch_kernel(true, norm_backward_kernel<T, V, 256, LAYER>, grid, 256, 0, st, p, part);

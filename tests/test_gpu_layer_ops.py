@@ -102,7 +102,9 @@ def near(got, want, bound, what):
 NORM_SHAPES = [(1, 1), (1, 896), (3, 8), (5, 7), (2, 33), (9, 257), (130, 128), (64, 1024), (33, 2056), (700, 1537),
                (17, 4096), (3, 5003), (5, 8192), (2, 8200), (3, 12288), (2, 16384), (2, 16400), (1, 20001), (1201, 64),
                # many rows of whole vectors: the backward pass's ring, of every width and number of slots
-               (700, 1024), (1300, 1032), (611, 2056), (777, 4096), (640, 8192), (3001, 256), (900, 512), (1000, 520), (2000, 896)]
+               (700, 1024), (1300, 1032), (611, 2056), (777, 4096), (640, 8192), (3001, 256), (900, 512), (1000, 520), (2000, 896),
+               # short rows, several to a warp, whole CTAs of them and one too many
+               (1, 64), (15, 128), (16, 128), (17, 120), (5000, 72), (4097, 128), (129, 33), (1000, 3)]
 
 
 @pytest.mark.parametrize("shape", NORM_SHAPES)
@@ -714,7 +716,7 @@ def test_a_wait_that_runs_out_is_reported(mp, rows):
 
 @pytest.mark.parametrize("kind", ["rms", "layer"])
 def test_a_norm_whose_ring_is_not_filled_is_reported(mp, kind):
-    x, dy, w = make((900, 2048), "bf16", 1), make((900, 2048), "bf16", 2), make((2048,), "bf16", 3)
+    x, dy, w = make((900, 4096), "bf16", 1), make((900, 4096), "bf16", 2), make((4096,), "bf16", 3)
     k = mp.MP_NORM_LAYER if kind == "layer" else mp.MP_NORM_RMS
     _, mean, rstd = mp.mp_norm(x, w, kind=k)
     want = mp.mp_norm_backward(dy, x, w, mean, rstd, kind=k)
