@@ -252,7 +252,13 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), (ROWT <= 32 ? 3 : 4) * backwar
       if (place(k) < p.cols) {
         xn[k] = load_pack<T, V>(x + place(k));
         dn[k] = load_pack<T, V>(dy + place(k));
-        if (kAddAhead && p.add) an[k] = load_pack<T, V>(static_cast<const T*>(p.add) + r * p.ldadd + place(k));
+        if (p.add) {
+          const T* add = static_cast<const T*>(p.add) + r * p.ldadd + place(k);
+          if (kAddAhead)
+            an[k] = load_pack<T, V>(add);
+          else if ((threadIdx.x * V * sizeof(T)) % 128 == 0)  // one lane to a line: to L2 at least
+            prefetch_l2(add);
+        }
       }
   };
   uint64_t r0 = (uint64_t)blockIdx.x * kRows;
@@ -346,8 +352,8 @@ __global__ void __launch_bounds__(cta_of<ROWT>(), (ROWT <= 32 ? 3 : 4) * backwar
 // rows; groups of ROWT threads, 16 columns each, take the rows in turn.  The groups' sums are added up in shared memory: one
 // part per CTA.  A row costs about 0.45 us of an SM besides its bytes, so that rows have to be long, and layer norms, whose two
 // sums per column leave the other kernel few registers, gain most (both sides in us, bf16 unless stated, 67 MB each of x and dy):
-// rows of 4 KB RMS 47 without and 60 with the ring, layer 71 and 65, fp32 layer with add 97 and 62; rows of 8 KB RMS with add 55 and
-// 53, layer 73 and 58, fp32 RMS with add 57 and 51.
+// rows of 4 KB RMS 47 without and 60 with the ring, layer 71 and 57; rows of 6 KB fp32 layer 53 and 45; rows of 8 KB RMS with add 55
+// and 53, layer 73 and 59, fp32 RMS with add 57 and 51.
 constexpr int kRingThreads = 512 + 32, kRingSlots = 16;
 template <typename T, int ROWT, bool LAYER>
 __global__ void __launch_bounds__(kRingThreads, 1) norm_backward_ring_kernel(const NormLaunch p, float* part, uint32_t slots,
