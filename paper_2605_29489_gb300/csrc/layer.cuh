@@ -58,6 +58,13 @@ struct Scratch {
 // stream, whichever that is, still ends: each starts with kernel_begin (or kernel_wait and kernel_release), and
 // touches no memory before that.  A chain of single-token products saves about 2 us on each.
 
+// Kernels with more than 48 KB of dynamic shared memory are all allowed the same, whatever a launch takes: the setting is the
+// process's, and another thread's launch between a setting of its own and the launch would find too little.
+constexpr size_t kMaxDynamicSmem = 224 * 1024;
+inline cudaError_t allow_smem(const void* kernel) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxDynamicSmem);
+}
+
 // ---- element access ----------------------------------------------------------------------------
 template <typename T>
 struct Elem;

@@ -1131,8 +1131,7 @@ template <typename... P, typename... A>
 cudaError_t launch_cluster(void (*k)(P...), unsigned grid, unsigned threads, unsigned cluster, size_t smem, cudaStream_t st,
                            const A&... a) {
   if (smem > 0) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = smem <= kMaxDynamicSmem ? allow_smem(reinterpret_cast<const void*>(k)) : cudaErrorInvalidValue;
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};

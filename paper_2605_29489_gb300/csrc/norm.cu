@@ -710,8 +710,7 @@ template <typename T, bool LAYER>
 cudaError_t norm_backward_ring(const NormLaunch& p, const RingPlan& r, float* part, cudaStream_t st) {
   const size_t smem = std::max<size_t>((size_t)r.slots * r.slot_bytes, 4u * kWideCols);
   auto go = [&](auto kernel) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel));
     if (e != cudaSuccess) return e;
     return launch_kernel(true, kernel, dim3(r.ctas), kRingThreads, smem, st, p, part, r.slots, p.cols * (uint32_t)sizeof(T));
   };

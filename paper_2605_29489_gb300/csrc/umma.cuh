@@ -72,7 +72,9 @@ __device__ __forceinline__ void umma_commit(uint64_t* bar) {
 
 // A kernel that takes tensor memory and may start before the one ahead of it has ended (launch_kernel) waits for
 // that end first, takes its memory, and only then lets the next one start: two kernels that wait for one another, one
-// for an end and one for columns, cannot come about, whatever kernels run ahead and behind.
+// for an end and one for columns, cannot come about, whatever kernels run ahead and behind.  Nor do such kernels on two streams
+// want more columns than an SM has: a CTA that takes all 512 leaves no shared memory for another one's stages, and as many of the
+// others as shared memory holds take 384 at most.
 __device__ __forceinline__ void kernel_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void kernel_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -452,6 +452,35 @@ def test_streams_and_graphs(mp):
     mp.mp_layer_status()
 
 
+def test_calls_from_many_threads(mp):
+    """threads whose products take different amounts of shared memory, each on a stream of its own"""
+    import concurrent.futures as cf
+
+    shapes = [(1, 4096, 512), (24, 1024, 300), (100, 700, 640), (300, 512, 2000), (1200, 256, 4096), (700, 4096, 64)]
+    cases = [linear_case("bf16", s, 3 + i) for i, s in enumerate(shapes)]
+    want = [mp.mp_linear(c["x"], c["w"])[0] for c in cases]
+    x, dy = make((900, 4096), "bf16", 1), make((900, 4096), "bf16", 2)
+    _, _, rstd = mp.mp_norm(x)
+    norm = mp.mp_norm_backward(dy, x, None, None, rstd)[0]
+    torch.cuda.synchronize()
+
+    def work(k):
+        s = torch.cuda.Stream()
+        for i in range(40):
+            c, w = cases[(i + k) % len(cases)], want[(i + k) % len(cases)]
+            with torch.cuda.stream(s):
+                y, _ = mp.mp_linear(c["x"], c["w"])
+                n = mp.mp_norm_backward(dy, x, None, None, rstd)[0] if i % 8 == 0 else norm
+            s.synchronize()
+            if not torch.equal(y, w) or not torch.equal(n, norm):
+                return (k, i)
+        return None
+
+    with cf.ThreadPoolExecutor(6) as ex:
+        assert [r for r in ex.map(work, range(6)) if r] == []
+    mp.mp_layer_status()
+
+
 def test_linear_far_into_large_matrices(mp):
     """rows beyond 2^32 bytes and 2^31 elements: the last rows of a tall bf16 matrix, forward and backward"""
     rows, k, n = (1 << 31) // 64 + 300, 64, 8
