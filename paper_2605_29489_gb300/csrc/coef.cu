@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(kThreads, 4) coef_kernel(const CoefLaunch p, f
   uint32_t mask = at < len ? p.mask[b] : 0u;
   const uint64_t off = p.blk_off[b] + at;
   const uint32_t n = at < len ? min(len - at, item) : 0u;
-  if (kChecked && !chunk_in_bounds(b, 0, p.n_blocks, p.blk_off[b], len, off, n, mask, p.K, sizeof(T), 0, p.ext)) {
+  if (kChecked && mask != 0u && !chunk_in_bounds(b, 0, p.n_blocks, p.blk_off[b], len, off, n, mask, p.K, sizeof(T), 0, p.ext)) {
     if (threadIdx.x == 0) atomicOr_system(p.err, kErrBounds);
     mask = 0u;
   }

@@ -771,3 +771,27 @@ def test_trace_ranges(mp):
     _, _, rstd = mp.mp_norm(y)
     kinds = [r["kind"] for r in mp.mp_trace_stop()]
     assert kinds == [mp.MP_TRACE_LINEAR, mp.MP_TRACE_NORM]
+
+
+def test_checked_build_of_the_coefficients_gradient():
+    """blocks of many items, ragged ends and omitted blocks through the checked library: no check fails, the same result"""
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = ("import sys; sys.path.insert(0, 'tests'); import torch, test_gpu_layer_ops as t, paper_2605_29489_gb300 as mp\n"
+            "fam, b, ex, g = t.coef_family(mp, 'bf16', [400000, 31, 16384, 16385], 65536, 8, 0.4, 5)\n"
+            "op = mp.make_op(mp.MP_OP_TA, alpha=[0.3] * 8)\n"
+            "idx = mp.mp_index_blocks(fam, op)\n"
+            "plan = mp.mp_plan(idx, op, mp.mp_budget_from_fraction(fam, 0.5))\n"
+            "out = mp.mp_coef_grad(fam, idx, plan, g)\n"
+            "mp.mp_layer_status()\n"
+            "print(mp.mp_version(), [v.hex() for v in out.flatten().tolist()])\n")
+    got = []
+    for checked in ("0", "1"):
+        r = subprocess.run([sys.executable, "-c", code], cwd=root, env=dict(os.environ, MERGEPIPE_CHECKED=checked),
+                           capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stdout + r.stderr
+        got.append(r.stdout)
+    assert "checked" in got[1] and got[0].split("[")[1] == got[1].split("[")[1]
