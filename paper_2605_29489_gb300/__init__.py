@@ -521,6 +521,18 @@ def _vector(name, t, n, dtype, device):
     return t.data_ptr()
 
 
+def _empty(stream, shape, dtype, where):
+    """a result's memory, from the stream that writes it: memory that the current stream has let go may still be in use
+    there.  The current stream may read the result, and the allocator waits for that when it is dropped.  A call's
+    inputs, and results that its caller passes, are the caller's to keep, as with every use of a tensor on another stream"""
+    if stream is None:
+        return _torch.empty(shape, dtype=dtype, device=where)
+    with _torch.cuda.stream(_torch.cuda.ExternalStream(_stream_ptr(stream), device=where)):
+        t = _torch.empty(shape, dtype=dtype, device=where)
+    t.record_stream(_torch.cuda.current_stream(where))
+    return t
+
+
 def _call(f, args, stream, device):
     rc = f(ctypes.byref(args), _raw_stream(device) if stream is None else _stream_ptr(stream))
     if rc != MP_OK:
@@ -533,9 +545,9 @@ def mp_norm(x, weight=None, bias=None, eps=1e-6, kind=MP_NORM_RMS, out=None, str
     torch, number, device, shape = _first(x)
     rows, cols = shape
     dt, where = x.dtype, x.device
-    y = torch.empty(shape, dtype=dt, device=where) if out is None else out
-    mean = torch.empty(rows, dtype=torch.float32, device=where) if kind == MP_NORM_LAYER else None
-    rstd = torch.empty(rows, dtype=torch.float32, device=where)
+    y = _empty(stream, shape, dt, where) if out is None else out
+    mean = _empty(stream, rows, torch.float32, where) if kind == MP_NORM_LAYER else None
+    rstd = _empty(stream, rows, torch.float32, where)
     _call((_lib or lib()).mp_norm,
           _NormArgs(number, kind, rows, cols, eps, *_matrix("x", x, shape, dt, device), *_matrix("out", y, shape, dt, device),
                     _vector("weight", weight, cols, dt, device), _vector("bias", bias, cols, dt, device),
@@ -550,9 +562,9 @@ def mp_norm_backward(dy, x, weight, mean, rstd, kind=MP_NORM_RMS, bias=False, ad
     rows, cols = shape
     dt, where = x.dtype, x.device
     if dx is None:
-        dx = torch.empty(shape, dtype=dt, device=where)
-    dw = None if weight is None else torch.empty(cols, dtype=dt, device=where)
-    db = torch.empty(cols, dtype=dt, device=where) if bias else None
+        dx = _empty(stream, shape, dt, where)
+    dw = None if weight is None else _empty(stream, cols, dt, where)
+    db = _empty(stream, cols, dt, where) if bias else None
     _call((_lib or lib()).mp_norm_backward,
           _NormBackwardArgs(number, kind, rows, cols, *_matrix("dy", dy, shape, dt, device),
                             *_matrix("x", x, shape, dt, device), *_matrix("add", add, shape, dt, device),
@@ -567,13 +579,13 @@ def mp_linear(x, w, bias=None, act=MP_ACT_NONE, mul=None, residual=None, keep_pr
     """(y, pre): y = act(z) * mul + residual, z = x w^T + bias, for x [rows, in] and w [out, in]; pre is z where
     keep_pre is set (the backward pass needs it with an activation or a factor), else None.  out: where y goes
     (may be mul or residual), else a new tensor"""
-    torch, number, device, xs = _first(x)
+    _, number, device, xs = _first(x)
     rows, k = xs
     n = _first(w, "w")[3][0]
     shape = (rows, n)
     dt, where = x.dtype, x.device
-    y = torch.empty(shape, dtype=dt, device=where) if out is None else out
-    pre = torch.empty(shape, dtype=dt, device=where) if keep_pre else None
+    y = _empty(stream, shape, dt, where) if out is None else out
+    pre = _empty(stream, shape, dt, where) if keep_pre else None
     _call((_lib or lib()).mp_linear,
           _LinearArgs(number, act, rows, k, n, *_matrix("x", x, xs, dt, device), *_matrix("w", w, (n, k), dt, device),
                       *_matrix("mul", mul, shape, dt, device), *_matrix("residual", residual, shape, dt, device),
@@ -586,7 +598,7 @@ def mp_linear_backward(dy, x, w, pre=None, act=MP_ACT_NONE, mul=None, bias=False
                        dw_add=None, dx=None, dw=None, stream=None):
     """(dx, dw, db, dmul) of mp_linear; db only where `bias` is set, dmul with a factor.  dx_add, dw_add: gradients
     to add to; dx, dw: where the results go (may be dx_add and dw_add), else new tensors"""
-    torch, number, device, xs = _first(x)
+    _, number, device, xs = _first(x)
     rows, k = xs
     n = _first(w, "w")[3][0]
     ws, shape = (n, k), (rows, n)
@@ -594,13 +606,13 @@ def mp_linear_backward(dy, x, w, pre=None, act=MP_ACT_NONE, mul=None, bias=False
     if not need_dx:
         dx = dx_add = None
     elif dx is None:
-        dx = torch.empty(xs, dtype=dt, device=where)
+        dx = _empty(stream, xs, dt, where)
     if not need_dw:
         dw = dw_add = None
     elif dw is None:
-        dw = torch.empty(ws, dtype=dt, device=where)
-    db = torch.empty(n, dtype=dt, device=where) if bias else None
-    dmul = None if mul is None else torch.empty(shape, dtype=dt, device=where)
+        dw = _empty(stream, ws, dt, where)
+    db = _empty(stream, n, dt, where) if bias else None
+    dmul = None if mul is None else _empty(stream, shape, dt, where)
     _call((_lib or lib()).mp_linear_backward,
           _LinearBackwardArgs(number, act, rows, k, n, *_matrix("dy", dy, shape, dt, device),
                               *_matrix("x", x, xs, dt, device), *_matrix("w", w, ws, dt, device),
@@ -621,7 +633,7 @@ def mp_coef_grad(fam: Family, index: Handle, plan: Handle, grad, out=None, strea
     if device < 0:
         raise ValueError("grad must be on a GPU")
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=grad.device)
+        out = _empty(stream, shape, torch.float32, grad.device)
     elif out.shape != shape or out.dtype != torch.float32 or not out.is_contiguous() or out.get_device() != device:
         raise ValueError(f"out must be {shape} contiguous elements of float32 on grad's GPU")
     span = fam.tensors[-1][0] + fam.tensors[-1][1]

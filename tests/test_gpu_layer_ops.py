@@ -452,6 +452,33 @@ def test_streams_and_graphs(mp):
     mp.mp_layer_status()
 
 
+def test_a_stream_that_is_not_the_current_one(mp):
+    """results of calls on another stream: dropped at once, they are not handed out again before that stream is done
+    with them: a fill on the current stream right after does not reach them, nor they it"""
+    c = linear_case("bf16", (2048, 2048, 2048), 3)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        for _ in range(20):
+            y, pre = mp.mp_linear(c["x"], c["w"], keep_pre=True, stream=stream)
+            del y, pre
+            z = torch.zeros((2048, 2048), dtype=torch.bfloat16, device="cuda")
+            torch.cuda.synchronize()
+            assert not z.any()
+    want, _ = mp.mp_linear(c["x"], c["w"])
+    torch.cuda.synchronize()
+    big = torch.empty(1 << 30, dtype=torch.uint8, device="cuda")
+    for _ in range(5):  # memory that the current stream still has to write is not a result's
+        z = torch.empty((2048, 2048), dtype=torch.bfloat16, device="cuda")
+        for _ in range(50):
+            big.zero_()
+        z.zero_()
+        del z
+        got, _ = mp.mp_linear(c["x"], c["w"], stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
 def test_calls_from_many_threads(mp):
     """threads whose products take different amounts of shared memory, each on a stream of its own"""
     import concurrent.futures as cf
